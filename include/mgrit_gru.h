@@ -257,6 +257,88 @@ int xent_head_fwd_bwd_noalloc(int32_t B, int32_t H, int32_t C, const float* hT, 
                               const int32_t* labels, float* loss, float* dhT, float* dWc, float* dbc,
                               mgrit_stream_t stream);
 
+/* ---- linear recurrences, token probabilities and distillation (additions; the paper has no counterpart) ----------------------
+ *
+ * Element types of the arrays marked `dtype` below.  States, statistics and losses are fp32 whatever the type; results of 16-bit
+ * type are rounded once, to nearest.  These calls need no alignment beyond an element's own size, and no array of theirs may
+ * overlap an output except where a call says so. */
+enum { MGRIT_F32 = 0, MGRIT_BF16 = 1, MGRIT_F16 = 2 };
+/* Value of gated_scan_args.cell besides MGRIT_CELL_CLASSIC and MGRIT_CELL_IMPLICIT: the coefficients themselves are given. */
+enum { MGRIT_SCAN_COEFFICIENTS = 2 };
+
+/* An array of T x B rows of H contiguous elements: row (t, b) starts at data + t * t_stride + b * b_stride (strides in
+ * elements, so time-major and batch-major arrays and slices of wider rows all serve; an input may repeat rows by a stride
+ * of zero, the rows of an output must not overlap: MGRIT_INVALID_ARG). */
+typedef struct { void* data; int64_t t_stride, b_stride; } mgrit_rows;
+
+/* Gated linear recurrence  h_t = a_t h_{t-1} + b_t, every unit for itself (all products element by element).  The
+ * coefficients come from two pre-activations g (gate) and c (candidate), z = sigmoid(g), n = tanh(c), by the cells of
+ * Eq. "gru-classic" and Eq. "gru-imap" with z in the place of 1 - z and without their recurrent matrix:
+ *   MGRIT_CELL_CLASSIC:      a = 1 - dt z,          b = dt z n
+ *   MGRIT_CELL_IMPLICIT:     a = 1 / (1 + dt z),    b = dt z n / (1 + dt z)
+ *   MGRIT_SCAN_COEFFICIENTS: a = g,                 b = c            (dt unused)
+ * Without the matrix the recurrence is linear in h, so one scan over time solves it exactly; there are no cycles.
+ *   lengths[B] (int32) or NULL: sequence b has steps 0 .. lengths[b] - 1 (values outside 0..T count as the nearest of the two).
+ *     Behind its end nothing is read, h and the gradients are written as zero, and the state stays what it was.
+ *   reset (rows of ONE uint8 each, H ignored) or data == NULL: where it is non-zero, h_{t-1} is taken as zero (a new sequence
+ *     starts in the same row).
+ *   h0[B,H] or NULL (zero); hT[B,H] or NULL: state after the last step of each sequence (h0 where it has none).  hT may be h0
+ *     itself: T = 1 is then one step of generation, with the state updated in place.
+ * Backward, at the GIVEN states h (what the forward call stored): dh_seed (rows) or data == NULL: loss derivative w.r.t. each
+ * stored h_t (not read behind a sequence's end); dhT[B,H] or NULL: w.r.t. the last state; one of the two must be given.
+ *   Outputs: dgate, dcand (rows), dh0[B,H] or NULL.
+ * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  B * H < 2^31, T < 2^31 - 1024. */
+typedef struct {
+  int32_t T, B, H;
+  int32_t cell;                 /* MGRIT_CELL_CLASSIC, MGRIT_CELL_IMPLICIT or MGRIT_SCAN_COEFFICIENTS */
+  int32_t dtype;                /* of gate, cand, h, dh_seed, dgate and dcand */
+  float dt;                     /* >= 0 */
+  mgrit_rows gate, cand, h;     /* both calls: [T,B,H]; the forward call writes h */
+  mgrit_rows reset;             /* uint8 [T,B] or data == NULL */
+  const float* h0; const int32_t* lengths;
+  float* hT;                    /* forward */
+  mgrit_rows dh_seed;           /* backward from here on */
+  const float* dhT;
+  mgrit_rows dgate, dcand;
+  float* dh0;
+} gated_scan_args;
+/* Workspace of both calls in bytes (device, 256-byte aligned; 0: none is needed, or the sizes are bad). */
+size_t gated_scan_workspace_bytes(int32_t T, int32_t B, int32_t H);
+int gated_scan_forward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream);
+int gated_scan_backward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream);
+
+/* Log probabilities of given tokens, with the entropy of each row's distribution and its `top` most probable tokens.
+ *   logits: N rows of V elements (dtype), row r at logits + r * ld (elements; ld >= V, 0 <= top <= min(V, 128)).
+ *   tokens[N] (int32) or NULL -> logprob[N] = x[token] - lse, 0 for a token outside [0, V) (a row without a target).
+ *   entropy[N] = - sum_v p_v log p_v and lse[N] = log sum_v exp x_v (each may be NULL);
+ *   top_logprob[N,top], top_id[N,top] (int32), falling; equal logits in rising order of their token (NULL where top == 0).
+ * A logit of -inf is a token that cannot occur: probability zero, log probability -inf.  A row of nothing else has no
+ * distribution: lse and all its log probabilities are -inf, its entropy 0.  A row with a NaN or +inf has NaN for all of its values
+ * but the ids (NaN ranks behind -inf there).
+ * token_logprobs_backward: dlogits_v = dlogprob ([v = token] - p_v) - dentropy p_v (log p_v + entropy), with p_v =
+ *   exp(x_v - lse) from the given statistics (of the forward call); tokens and dlogprob, or entropy and dentropy, may be NULL
+ *   together, not all four; the token's term is absent for a token outside [0, V); where p_v is 0 so is its term; rows whose
+ *   lse is -inf get zeros.  dlogits: N rows at dlogits + r * dld; it may be the logits array itself (same ld: in place). */
+int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int64_t ld, const int32_t* tokens, int32_t top,
+                   float* logprob, float* entropy, float* lse, float* top_logprob, int32_t* top_id, mgrit_stream_t stream);
+int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* logits, int64_t ld, const int32_t* tokens,
+                            const float* lse, const float* entropy, const float* dlogprob, const float* dentropy,
+                            void* dlogits, int64_t dld, mgrit_stream_t stream);
+
+/* Distillation from a teacher's top logits: loss, and its gradient w.r.t. the student's logits, in one call.
+ *   logits as above; top_id[N,K] (int32), top_logit[N,K]: the teacher's K best tokens of each row and their logits (or log
+ *   probabilities: a constant of the row drops out), 1 <= K <= 1024.  With q = softmax(x / tau) over V and p = softmax(y / tau)
+ *   over the row's K alternatives:   row_loss = tau^2 sum_k p_k (log p_k - log q[id_k]),   loss[1] = sum_r w_r row_loss_r,
+ *   dlogits = w_r tau (q - p at the ids).   weight[N] or NULL: w_r, 1/N without it (the mean).
+ * An id outside [0, V) or a teacher logit of -inf is an absent alternative (p = 0); a row without any has loss 0 and gradient 0; an id
+ * may occur twice, its probabilities then add up in the gradient.  A student logit of -inf has q = 0: where the teacher gives that token
+ * a probability the loss is +inf and the gradient stays finite.  NaN, or +inf, of either side makes its row's loss and gradient NaN.
+ * A row of weight zero has gradient zero whatever it holds, and adds nothing to loss.
+ * row_loss[N] is required; sums run in a fixed order.  dlogits may be the logits array itself (same ld: in place). */
+int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float tau, const void* logits, int64_t ld,
+                         const int32_t* top_id, const float* top_logit, const float* weight, float* loss, float* row_loss,
+                         void* dlogits, int64_t dld, mgrit_stream_t stream);
+
 /* Theta <- Theta - lr * g (last line of Algorithm "MGRITTraining"); n fp32 elements. */
 int sgd_update(float* p, const float* g, size_t n, float lr, mgrit_stream_t stream);
 

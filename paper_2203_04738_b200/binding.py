@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -25,6 +26,8 @@ RELAX_F, RELAX_FCF, RELAX_FCFCF = 0, 1, 2
 OPERANDS_FP32, OPERANDS_TF32, OPERANDS_BF16, OPERANDS_TF32_1PASS = 0, 1, 2, 3
 FLAG_SKIP_DUPLICATE_FRELAX, FLAG_F_CYCLE, FLAG_RAGGED_T, FLAG_GI_CARRIES_COPIES, FLAG_GI_F32_UNUSED = 1, 2, 4, 8, 16
 FLAG_H_LEADS_WITH_H0 = 32
+SCAN_COEFFICIENTS = 2                      # `cell` of the gated scan: gate and candidate are the coefficients themselves
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class Cfg(ctypes.Structure):
@@ -70,6 +73,13 @@ lib.xent_head_fwd_bwd.argtypes = [_i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp
 lib.xent_head_fwd_bwd_noalloc.argtypes = [_i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 lib.sgd_update.argtypes = [_vp, _vp, _sz, ctypes.c_float, _vp]
 lib.adam_update.argtypes = [_vp, _vp, _vp, _vp, _sz, ctypes.c_float, ctypes.c_float, ctypes.c_float, ctypes.c_float, _i32, _vp]
+lib.gated_scan_workspace_bytes.argtypes = [_i32, _i32, _i32]
+lib.gated_scan_workspace_bytes.restype = _sz
+lib.gated_scan_forward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
+lib.gated_scan_backward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
+lib.token_logprobs.argtypes = [_i32, _i32, _i32, _vp, ctypes.c_int64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.token_logprobs_backward.argtypes = [_i32, _i32, _i32, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]
+lib.distill_topk_fwd_bwd.argtypes = [_i32, _i32, _i32, _i32, ctypes.c_float, _vp, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]
 lib.mgrit_gru_selftest_bounded_wait.argtypes = [_i32, _vp]
 lib.mgrit_gru_last_device_status.restype = ctypes.c_int
 lib.mgrit_gru_clear_device_status.restype = ctypes.c_int
@@ -356,6 +366,168 @@ def xent_head_fwd_bwd_noalloc(hT, Wc, bc, labels, out=None):
     _check(lib.xent_head_fwd_bwd_noalloc(B, H, C, _f32(hT), _f32(Wc), _f32(bc), _ptr(labels), _f32(loss), _f32(dhT), _f32(dWc),
                                          _f32(dbc), _stream()))
     return loss, dhT, dWc, dbc
+
+
+# ---- linear recurrences, token probabilities, distillation: arrays of fp32, bf16 or fp16, any strides with contiguous rows ----------
+
+def _require(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dtype(t):
+    code = _DTYPES.get(t.dtype)
+    _require(code is not None, f"fp32, bf16 or fp16 required, got {t.dtype}")
+    return code
+
+
+def _on_device(dev, fn, *args):
+    """fn(*args, stream) on the current stream of `dev`, whatever device is current."""
+    if torch.cuda.current_device() == dev.index:
+        return _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    with torch.cuda.device(dev):
+        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+
+
+def _like(t, dev, shape, dtype, name):
+    """Address of a contiguous array of that device, shape and type (0: not given)."""
+    if t is None:
+        return 0
+    _require(t.device == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous(),
+             f"{name}: contiguous {dtype} array of shape {tuple(shape)} on {dev} required")
+    return t.data_ptr()
+
+
+def _strided(t, like, name):
+    """(address, stride of t, stride of b) of an array of the shape, type and device of `like`."""
+    if t is None:
+        return 0, 0, 0
+    _require(t.shape == like.shape and t.dtype == like.dtype and t.device == like.device, f"{name}: {like.dtype} array of shape {tuple(like.shape)} on {like.device} required")
+    st = t.stride()
+    _require(st[2] == 1 or t.shape[2] == 1, f"{name}: the units of a row must be contiguous")
+    return t.data_ptr(), st[0], st[1]
+
+
+_SCAN_ARGS = struct.Struct("@5if" + 3 * "Pqq" + "Pqq" + "PPP" + "Pqq" + "P" + 2 * "Pqq" + "P")      # gated_scan_args
+
+
+def _scan_args(gate, cand, h, reset, lengths, h0, cell, dt):
+    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
+    T, Bn, H = gate.shape
+    dev = gate.device
+    if reset is not None:
+        _require(reset.dtype in (torch.uint8, torch.bool) and reset.shape == (T, Bn) and reset.device == dev, f"reset: uint8 or bool array [T,B] on {dev} required")
+        r = (reset.data_ptr(), *reset.stride())
+    else:
+        r = (0, 0, 0)
+    return (T, Bn, H, cell, _dtype(gate), dt, *_strided(gate, gate, "gate"), *_strided(cand, gate, "cand"), *_strided(h, gate, "h"), *r,
+            _like(h0, dev, (Bn, H), torch.float32, "h0"), _like(lengths, dev, (Bn,), torch.int32, "lengths"))
+
+
+def _scan_ws(T, Bn, H, ws, dev):
+    n = lib.gated_scan_workspace_bytes(T, Bn, H)
+    if n == 0:
+        return None, 0
+    if ws is None or ws.numel() < n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _require(ws.device == dev and ws.dtype == torch.uint8 and ws.is_contiguous(), f"ws: contiguous uint8 array on {dev} required")
+    return ws.data_ptr(), ws.numel()
+
+
+def gated_scan_forward(gate, cand, h0=None, cell=CELL_IMPLICIT, dt=1.0, lengths=None, reset=None, h=None, hT=None, ws=None):
+    """Gated linear recurrence h_t = a_t h_{t-1} + b_t over gate[T,B,H] and cand[T,B,H] (fp32, bf16 or fp16; any strides with contiguous
+    units, so time-major or batch-major arrays and halves of one projection serve) -> (h[T,B,H] of the same type, hT[B,H] fp32).
+    cell: CELL_CLASSIC, CELL_IMPLICIT (a, b from sigmoid(gate) and tanh(cand)) or SCAN_COEFFICIENTS (a = gate, b = cand).
+    h0[B,H] fp32; lengths[B] int32; reset[T,B] uint8 or bool: the sequence starts anew there.  hT may be h0: one call with T = 1 is a step
+    of generation that updates the state in place.  Behind a sequence's end h is zero and hT keeps the state."""
+    dev = gate.device
+    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
+    T, Bn, H = gate.shape
+    h = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if h is None else h
+    hT = torch.empty(Bn, H, device=dev) if hT is None else hT
+    args = _scan_args(gate, cand, h, reset, lengths, h0, cell, dt)
+    packed = _SCAN_ARGS.pack(*args, _like(hT, dev, (Bn, H), torch.float32, "hT"), *(0,) * 11)
+    _on_device(dev, lib.gated_scan_forward, packed, *_scan_ws(T, Bn, H, ws, dev))
+    return h, hT
+
+
+def gated_scan_backward(gate, cand, h, h0=None, dh_seed=None, dhT=None, cell=CELL_IMPLICIT, dt=1.0, lengths=None, reset=None, dgate=None,
+                        dcand=None, dh0=None, ws=None):
+    """Gradients of gated_scan_forward at its states h, given dh_seed[T,B,H] (w.r.t. every h_t) and / or dhT[B,H] (w.r.t. hT)
+    -> (dgate, dcand, dh0[B,H] fp32)."""
+    dev = gate.device
+    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
+    T, Bn, H = gate.shape
+    dgate = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if dgate is None else dgate
+    dcand = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if dcand is None else dcand
+    dh0 = torch.empty(Bn, H, device=dev) if dh0 is None else dh0
+    args = _scan_args(gate, cand, h, reset, lengths, h0, cell, dt)
+    packed = _SCAN_ARGS.pack(*args, 0, *_strided(dh_seed, gate, "dh_seed"), _like(dhT, dev, (Bn, H), torch.float32, "dhT"), *_strided(dgate, gate, "dgate"),
+                             *_strided(dcand, gate, "dcand"), _like(dh0, dev, (Bn, H), torch.float32, "dh0"))
+    _on_device(dev, lib.gated_scan_backward, packed, *_scan_ws(T, Bn, H, ws, dev))
+    return dgate, dcand, dh0
+
+
+@dataclass
+class TokenLogprobs:
+    logprob: torch.Tensor | None
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logprob: torch.Tensor | None
+    top_id: torch.Tensor | None
+
+
+def _logit_rows(t, name, like=None):
+    """(address, elements from row to row) of a matrix of logits with contiguous rows."""
+    _require(t.dim() == 2 and t.is_cuda and (like is None or (t.shape == like.shape and t.dtype == like.dtype and t.device == like.device)),
+             f"{name}: CUDA matrix [N,V] required" + ("" if like is None else ", of the logits' shape, type and device"))
+    _require(t.stride(1) == 1 or t.shape[1] == 1, f"{name}: the elements of a row must be contiguous")
+    return t.data_ptr(), t.stride(0)
+
+
+def token_logprobs(logits, tokens=None, top=0, out=None):
+    """Log probabilities of tokens[N] (int32) under the rows of logits[N,V] (fp32, bf16 or fp16), the entropy and the log of the sum of
+    exponentials of each row, and its `top` most probable tokens (equal logits: the lower token first; top <= 128)
+    -> TokenLogprobs of fp32 arrays (top_id int32).  `out`: a TokenLogprobs of an earlier call of the same sizes, to be overwritten."""
+    p, ld = _logit_rows(logits, "logits")
+    (N, V), dev, f32 = logits.shape, logits.device, torch.float32
+    if out is None:
+        out = TokenLogprobs(None if tokens is None else torch.empty(N, device=dev), torch.empty(N, device=dev), torch.empty(N, device=dev),
+                            torch.empty(N, top, device=dev) if top > 0 else None, torch.empty(N, top, dtype=torch.int32, device=dev) if top > 0 else None)
+    _on_device(dev, lib.token_logprobs, N, V, _dtype(logits), p, ld, _like(tokens, dev, (N,), torch.int32, "tokens"), top,
+               _like(out.logprob, dev, (N,), f32, "logprob"), _like(out.entropy, dev, (N,), f32, "entropy"), _like(out.lse, dev, (N,), f32, "lse"),
+               _like(out.top_logprob, dev, (N, top), f32, "top_logprob"), _like(out.top_id, dev, (N, top), torch.int32, "top_id"))
+    return out
+
+
+def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogprob=None, dentropy=None, dlogits=None):
+    """Gradient w.r.t. the logits, given those w.r.t. the tokens' log probabilities and / or the entropies and the statistics that the
+    forward call returned.  dlogits may be the logits themselves (in place).  -> dlogits[N,V]"""
+    p, ld = _logit_rows(logits, "logits")
+    (N, V), dev, f32 = logits.shape, logits.device, torch.float32
+    dlogits = torch.empty(N, V, dtype=logits.dtype, device=dev) if dlogits is None else dlogits
+    d, dld = _logit_rows(dlogits, "dlogits", logits)
+    _on_device(dev, lib.token_logprobs_backward, N, V, _dtype(logits), p, ld, _like(tokens, dev, (N,), torch.int32, "tokens") if dlogprob is not None else 0,
+               _like(lse, dev, (N,), f32, "lse"), _like(entropy, dev, (N,), f32, "entropy") if dentropy is not None else 0,
+               _like(dlogprob, dev, (N,), f32, "dlogprob"), _like(dentropy, dev, (N,), f32, "dentropy"), d, dld)
+    return dlogits
+
+
+def distill_topk_fwd_bwd(logits, top_id, top_logit, weight=None, temperature=1.0, dlogits=None, loss=None, row_loss=None):
+    """Distillation of the rows of logits[N,V] from a teacher's top_id[N,K] (int32) and top_logit[N,K] (logits or log probabilities, as
+    token_logprobs returns them): -> (loss[1], row_loss[N], dlogits[N,V]).  weight[N]: of the rows (the mean without it).
+    dlogits may be the logits themselves (in place)."""
+    p, ld = _logit_rows(logits, "logits")
+    _require(top_id.dim() == 2, "top_id: matrix [N,K] required")
+    (N, V), K, dev, f32 = logits.shape, top_id.shape[1], logits.device, torch.float32
+    dlogits = torch.empty(N, V, dtype=logits.dtype, device=dev) if dlogits is None else dlogits
+    d, dld = _logit_rows(dlogits, "dlogits", logits)
+    loss = torch.empty(1, device=dev) if loss is None else loss
+    row_loss = torch.empty(N, device=dev) if row_loss is None else row_loss
+    _on_device(dev, lib.distill_topk_fwd_bwd, N, V, K, _dtype(logits), temperature, p, ld, _like(top_id, dev, (N, K), torch.int32, "top_id"),
+               _like(top_logit, dev, (N, K), f32, "top_logit"), _like(weight, dev, (N,), f32, "weight"), _like(loss, dev, (1,), f32, "loss"),
+               _like(row_loss, dev, (N,), f32, "row_loss"), d, dld)
+    return loss, row_loss, dlogits
 
 
 def sgd_update(p, g, lr):
