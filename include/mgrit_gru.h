@@ -287,12 +287,13 @@ typedef struct { void* data; int64_t t_stride, b_stride; } mgrit_rows;
  * Backward, at the GIVEN states h (what the forward call stored): dh_seed (rows) or data == NULL: loss derivative w.r.t. each
  * stored h_t (not read behind a sequence's end); dhT[B,H] or NULL: w.r.t. the last state; one of the two must be given.
  *   Outputs: dgate, dcand (rows), dh0[B,H] or NULL.
- * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  B * H < 2^31, T < 2^31 - 1024. */
+ * A gate or candidate of NaN makes its step's state NaN (and the gradients of its step and of those before it).
+ * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  B * H < 2^31, T < 2^31 - 1024, tiles of 64 steps x 32 units < 2^31. */
 typedef struct {
   int32_t T, B, H;
   int32_t cell;                 /* MGRIT_CELL_CLASSIC, MGRIT_CELL_IMPLICIT or MGRIT_SCAN_COEFFICIENTS */
   int32_t dtype;                /* of gate, cand, h, dh_seed, dgate and dcand */
-  float dt;                     /* >= 0 */
+  float dt;                     /* 0 .. 1e18 */
   mgrit_rows gate, cand, h;     /* both calls: [T,B,H]; the forward call writes h */
   mgrit_rows reset;             /* uint8 [T,B] or data == NULL */
   const float* h0; const int32_t* lengths;

@@ -760,7 +760,7 @@ int finish(cudaStream_t s, bool sync) {
   if (sync && cudaStreamSynchronize(s) != cudaSuccess) return MGRIT_CUDA_ERROR;
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) { fprintf(stderr, "mgrit_gru: CUDA error: %s\n", cudaGetErrorString(e)); return MGRIT_CUDA_ERROR; }
-  if (sync && (umma_device_status() != 0 || serial_device_status() != 0 || f32_device_status() != 0)) return MGRIT_DEVICE_TIMEOUT;
+  if (sync && (umma_device_status() != 0 || serial_device_status() != 0 || f32_device_status() != 0 || scan_device_status() != 0)) return MGRIT_DEVICE_TIMEOUT;
   return MGRIT_OK;
 }
 
@@ -2017,12 +2017,13 @@ int adam_update(float* p, const float* g, float* m, float* v, size_t n, float lr
 
 int mgrit_gru_last_device_status(void) {
   if (cudaDeviceSynchronize() != cudaSuccess) return MGRIT_CUDA_ERROR;
-  return (umma_device_status() != 0 || serial_device_status() != 0 || f32_device_status() != 0) ? MGRIT_DEVICE_TIMEOUT : MGRIT_OK;
+  return (umma_device_status() != 0 || serial_device_status() != 0 || f32_device_status() != 0 || scan_device_status() != 0) ? MGRIT_DEVICE_TIMEOUT : MGRIT_OK;
 }
 
 int mgrit_gru_clear_device_status(void) {
   if (cudaDeviceSynchronize() != cudaSuccess) return MGRIT_CUDA_ERROR;
-  return (umma_clear_device_status() == 0 && serial_clear_device_status() == 0 && f32_clear_device_status() == 0) ? MGRIT_OK : MGRIT_CUDA_ERROR;
+  return (umma_clear_device_status() == 0 && serial_clear_device_status() == 0 && f32_clear_device_status() == 0 &&
+          scan_clear_device_status() == 0) ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
 int mgrit_gru_selftest_bounded_wait(int32_t limit_ms, mgrit_stream_t stream) { return umma_selftest_wait(limit_ms, (cudaStream_t)stream); }

@@ -272,4 +272,8 @@ void stream_sgd(float* p, const float* g, size_t n, float lr, cudaStream_t s);
 void stream_adam(float* p, const float* g, float* m, float* v, size_t n, float lr, float b1, float b2, float eps, int step,
                  cudaStream_t s);
 
+// status word of the gated scan's bounded waits (scan_kernels.cu)
+int scan_device_status();
+int scan_clear_device_status();
+
 }  // namespace mg
