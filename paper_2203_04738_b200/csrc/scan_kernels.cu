@@ -4,16 +4,21 @@
 // bound by HBM as long as enough of the time axis is in flight at once.  Two kernels:
 //
 //  * scan_short_kernel, T <= kShort: a thread walks its columns.  One step of generation is this kernel: a launch and a trip to memory.
-//  * scan_tile_kernel: the time axis is cut into tiles of kSteps x kWarps steps and 32 x VC columns.  A thread holds kSteps steps of VC
+//  * scan_tile_kernel: the time axis is cut into tiles of S x kWarps steps and 32 x VC columns.  A thread holds S steps of VC
 //    columns in registers from the only time they are read to the time the results are written.  It reduces them to one pair
 //    (A, B): h_out = A h_in + B; the pairs of a tile's warps meet in shared memory, those of the tiles in the workspace.  A tile
 //    publishes its pair as soon as it has it; the state in front of a tile is the last published state before it, carried
-//    through the pairs of the tiles in between (decoupled look-back), and is published in turn.  Tiles are handed out by a counter,
-//    earlier times first, so whatever a tile waits for has been started before it, and the wait ends; it is bounded all the same.
+//    through the pairs of the tiles in between (decoupled look-back), and is published in turn.  Blocks stay and take tiles from a
+//    counter, earlier times first, each in the order in which it got them: the first unfinished tile waits for nothing, so every wait
+//    ends; it is bounded all the same.  While a block works on a tile the loads of its next one are in flight.
 //    The state is carried through the pairs one after the other, by the operation that the tiles themselves would have used, so that the
 //    bits do not depend on how far a tile had to look back.
+//    Published words are their own flags: the workspace is filled with a bit pattern that no result has, a word that
+//    differs from it is there.  So publishing is a plain store and looking one trip to L2, without fences.
 //
 // Backward is the same scan from the last step to the first: mu_t = a_t (seed_t + mu_{t+1}).
+#include <type_traits>
+
 #include "elem.cuh"
 
 namespace mg {
@@ -25,368 +30,612 @@ int* g_scan_status_ptrs[kMaxDevices] = {nullptr};
 struct ScanRows { char* p; i64 ts, bs; };      // strides in elements
 struct ScanArgs {
   int T, B, H;
-  float dt;
+  float dt, K, L;                              // gate: q = dt / (K + E), a = (L + E) / (K + E); see coefficients()
   ScanRows gate, cand, h, seed, dgate, dcand, reset;
   const float* h0; const int32_t* lengths; float* hT;
   const float* dhT; float* dh0;
   // tiles: nk along time, nc along the columns
-  int nk, nc;
-  unsigned* ticket; int* flags; float2* pairs; float* states; int* status;
+  int nk, nc, deep;
+  unsigned* ticket; float* states; unsigned long long* pairs; int* status;      // [nk][nc * 32 VC] each
 };
 
 constexpr int kShort = 8;                      // steps that one thread walks
 constexpr int kShortThreads = 128;
-constexpr int kSteps = 8, kWarps = 8, kTileSteps = kSteps * kWarps;
-constexpr int kLook = 4;                       // flags that a lane looks at: 128 tiles back
+#ifndef SCAN_W
+#define SCAN_W 8
+#endif
+#ifndef SCAN_V1
+#define SCAN_V1 1
+#endif
+#ifndef SCAN_SF
+#define SCAN_SF 16
+#endif
+#ifndef SCAN_SB
+#define SCAN_SB 8
+#endif
+#ifndef SCAN_BF
+#define SCAN_BF 1
+#endif
+#ifndef SCAN_BB
+#define SCAN_BB 1
+#endif
+constexpr int kWarps = SCAN_W;
+// Columns of a thread: 8 bytes of a row, or one where the rows do not allow that.  Its steps: what its registers hold twice (coefficients of
+// this tile, raw values of the next).
+template <class T> constexpr int kWide = 8 / sizeof(T);
+template <int VC, bool BACK> constexpr int kStepsOf = (BACK ? SCAN_SB : SCAN_SF) * (VC == 1 ? SCAN_V1 : 1);
+template <bool BACK> constexpr int kBlocksOf = BACK ? SCAN_BB : SCAN_BF;
+#ifndef SCAN_D
+#define SCAN_D 1
+#endif
+constexpr int kAhead = SCAN_D;                 // tiles whose loads are in flight behind the one in work
+constexpr int kLook = 4;                       // looks of 32 tiles back
+constexpr int kPairs = 2;                      // pairs of a column in flight in a look-back
 constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
 constexpr float kMaxDt = 1e18f;
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp_exact(float x) { const float y = rcp(x); return fmaf(fmaf(-x, y, 1.0f), y, y); }      // one Newton step
-__device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
-// a, b and, for the derivatives, z, 1 - z, n and r (implicit: 1 / (1 + dt z), classic: 1) of one element.
-// With E = e^-g and F = e^2c:  z = 1 / (1 + E), n = (F - 1) / (F + 1), 1 / (1 + dt z) = (1 + E) / (1 + E + dt); 1 - z = E z and
-// 1 - dt z = ((1 - dt) + E) z lose nothing where z is near 1.  Small candidates take the first terms of the tangent's series, since F - 1
-// would lose their digits (|c| < 0.1: the term left out is 5e-8 of the value).  E stops at e^40 (z = 4e-18) and F at e^20 (n = 1).
-// 16-bit types: both quotients from one reciprocal, since four of these operations an element take as long as its bytes (16 a cycle
-// and SM: 67 M elements in 65 us, the bytes in 61); what that costs is two roundings of fp32.
-struct Coef { float a, b, z, omz, n, r; };
-template <int CELL, bool FAST> __device__ __forceinline__ Coef coefficients(float g, float c, float dt) {
-  Coef o;
-  if (CELL == MGRIT_SCAN_COEFFICIENTS) { o.a = g; o.b = c; o.z = o.omz = o.n = o.r = 0.f; return o; }
-  const float E = ex2(min_nan(-g, 40.0f) * 1.44269504f), F = ex2(min_nan(c, 10.0f) * 2.88539008f);
-  const float P = CELL == MGRIT_CELL_CLASSIC ? 1.0f + E : (1.0f + E) + dt, Q = 1.0f + F;
-  float ip, iq;
+#ifndef SCAN_SCALAR
+#define SCAN_SCALAR 0
+#endif
+// VC columns side by side.  Two of them use the packed fp32 instructions, which take one issue slot for both: the scan of 16-bit types
+// is bound by instructions (55 an element of 6 bytes before this and the wider loads, 170 us where the bytes take 61).
+template <int VC> struct F {
+  float x[VC];
+  __device__ __forceinline__ static F all(float v) {
+    F f;
+#pragma unroll
+    for (int i = 0; i < VC; ++i) f.x[i] = v;
+    return f;
+  }
+  __device__ __forceinline__ float& at(int i) { return x[i]; }
+  __device__ __forceinline__ float at(int i) const { return x[i]; }
+};
+template <int VC> __device__ __forceinline__ F<VC> operator*(const F<VC>& a, const F<VC>& b) {
+  F<VC> r;
+  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = a.x[i] * b.x[i]; return r; }
+#pragma unroll
+  for (int i = 0; i + 1 < VC; i += 2)
+    asm("{.reg .b64 p, q, r; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; mul.rn.f32x2 r, p, q; mov.b64 {%0, %1}, r;}"
+        : "=f"(r.x[i]), "=f"(r.x[i + 1]) : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]));
+  return r;
+}
+template <int VC> __device__ __forceinline__ F<VC> operator+(const F<VC>& a, const F<VC>& b) {
+  F<VC> r;
+  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = a.x[i] + b.x[i]; return r; }
+#pragma unroll
+  for (int i = 0; i + 1 < VC; i += 2)
+    asm("{.reg .b64 p, q, r; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; add.rn.f32x2 r, p, q; mov.b64 {%0, %1}, r;}"
+        : "=f"(r.x[i]), "=f"(r.x[i + 1]) : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]));
+  return r;
+}
+template <int VC> __device__ __forceinline__ F<VC> fma_(const F<VC>& a, const F<VC>& b, const F<VC>& c) {
+  F<VC> r;
+  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = fmaf(a.x[i], b.x[i], c.x[i]); return r; }
+#pragma unroll
+  for (int i = 0; i + 1 < VC; i += 2)
+    asm("{.reg .b64 p, q, r, s; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; mov.b64 r, {%6, %7}; fma.rn.f32x2 s, p, q, r; mov.b64 {%0, %1}, s;}"
+        : "=f"(r.x[i]), "=f"(r.x[i + 1])
+        : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]), "f"(c.x[i]), "f"(c.x[i + 1]));
+  return r;
+}
+template <int VC, class Fn> __device__ __forceinline__ F<VC> each(F<VC> a, Fn&& fn) {
+  F<VC> r;
+#pragma unroll
+  for (int i = 0; i < VC; ++i) r.at(i) = fn(a.at(i), i);
+  return r;
+}
+
+// VC consecutive elements of a row, moved as one word
+template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
+  T x[VC];
+  __device__ __forceinline__ F<VC> get() const {
+    F<VC> f;
+#pragma unroll
+    for (int i = 0; i < VC; ++i) f.x[i] = to_f32(x[i]);
+    return f;
+  }
+  __device__ __forceinline__ void set(const F<VC>& f) {
+#pragma unroll
+    for (int i = 0; i < VC; ++i) x[i] = from_f32<T>(f.x[i]);
+  }
+};
+// the same, no lower than -40 (gates) or no higher than 10 (candidates); NaN stays.  Two 16-bit values take one instruction.
+template <bool GATE> __device__ __forceinline__ float clamped(float v) { float y; if (GATE) asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-40.f)); else asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(10.f)); return y; }
+template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; if (GATE) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc220c220u)); else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x41204120u)); return y; }
+template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; if (GATE) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd100d100u)); else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x49004900u)); return y; }
+template <bool GATE, class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Vec<T, VC>& x) {
+  if constexpr (sizeof(T) == 2 && VC % 2 == 0) {
+    Vec<T, VC> y;
+    const unsigned* in = reinterpret_cast<const unsigned*>(&x);
+    unsigned* out = reinterpret_cast<unsigned*>(&y);
+#pragma unroll
+    for (int i = 0; i < VC / 2; ++i) out[i] = clamped2<GATE>(in[i], T{});
+    return y.get();
+  } else {
+    F<VC> f = x.get();
+#pragma unroll
+    for (int i = 0; i < VC; ++i) f.x[i] = clamped<GATE>(f.x[i]);
+    return f;
+  }
+}
+template <class T, int VC> __device__ __forceinline__ Vec<T, VC> load(const T* p) { return *reinterpret_cast<const Vec<T, VC>*>(p); }
+template <class T, int VC> __device__ __forceinline__ void store(T* p, F<VC> f) {
+  Vec<T, VC> v;
+  v.set(f);
+  *reinterpret_cast<Vec<T, VC>*>(p) = v;
+}
+template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
+  Vec<T, VC> v;
+  v.set(F<VC>::all(0.f));
+  return v;
+}
+// The coefficients, and what their derivatives need.  With E = e^-g, G = e^2c and z = 1 / (1 + E):
+//   n = (G - 1) / (G + 1),  q = dt / (K + E),  a = 1 - q = (L + E) / (K + E),  b = q n
+// is the classic cell (q = dt z) for K = 1, L = 1 - dt and the implicit one (q = dt z / (1 + dt z)) for K = 1 + dt, L = 1, and in both
+//   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2).
+// Small candidates take the first terms of the tangent's series, since G - 1 would lose their digits.  E stops at e^40 and G at e^20,
+// where z is 4e-18 and n is 1.
+// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, the series' first term for |c| < 2^-9 (left out: 1.3e-6 of the
+// value).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
+// bytes 61).  The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
+// coefficients are right to a few units in the last place; two terms of the series for |c| < 0.1 (left out: 5e-8).
+template <int VC> struct Coef { F<VC> a, b, q, n, e; };      // e = E / (K + E)
+template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
+  constexpr bool FAST = sizeof(T) == 2;
+  Coef<VC> o;
+  using V = F<VC>;
+  if (GIVEN) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = V::all(0.f); return o; }
+  const V one = V::all(1.0f), g = get_clamped<true>(graw), c = get_clamped<false>(craw);
+  const V E = each(g * V::all(-1.44269504f), [](float v, int) { return ex2(v); }), G = each(c * V::all(2.88539008f), [](float v, int) { return ex2(v); });
+  const V P = E + V::all(s.K), Q = G + one;
+  V ip, iq;
   if (FAST) {
-    const float R = rcp(P * Q);
+    const V R = each(P * Q, [](float v, int) { return rcp(v); });
     ip = Q * R;
     iq = P * R;
   } else {
-    ip = rcp_exact(P);
-    iq = rcp_exact(Q);
+    ip = each(P, [](float v, int) { return rcp_exact(v); });
+    iq = each(Q, [](float v, int) { return rcp_exact(v); });
   }
-  const float c2 = c * c;
-  o.n = fabsf(c) < 0.1f ? c * fmaf(c2, fmaf(c2, 0.13333334f, -0.33333334f), 1.0f) : (F - 1.0f) * iq;
-  if (CELL == MGRIT_CELL_CLASSIC) {
-    o.z = ip;
-    o.omz = E * ip;
-    o.r = 1.0f;
-    o.a = ((1.0f - dt) + E) * ip;
-    o.b = dt * ip * o.n;
+  o.n = (G + V::all(-1.0f)) * iq;
+  if (FAST) {
+    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.001953125f ? c.at(i) : v; });
   } else {
-    o.r = o.a = (1.0f + E) * ip;
-    o.b = dt * ip * o.n;                       // dt z r = dt / (1 + E + dt)
-    o.z = FAST ? rcp(1.0f + E) : rcp_exact(1.0f + E);
-    o.omz = E * o.z;
+    const V c2 = c * c, small = c * fma_(c2, fma_(c2, V::all(0.13333334f), V::all(-0.33333334f)), one);
+    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.1f ? small.at(i) : v; });
   }
+  o.q = ip * V::all(s.dt);
+  o.a = FAST ? fma_(o.q, V::all(-1.0f), one) : (E + V::all(s.L)) * ip;
+  o.b = o.q * o.n;
+  o.e = E * ip;
   return o;
 }
-
 // d(gate), d(cand) of a step whose state has the derivative 1
-template <int CELL> __device__ __forceinline__ void slopes(const Coef& k, float hp, float dt, float& wg, float& wc) {
-  if (CELL == MGRIT_SCAN_COEFFICIENTS) { wg = hp; wc = 1.0f; return; }
-  const float s = dt * k.z * k.r;
-  wg = s * k.r * (k.n - hp) * k.omz;
-  wc = s * (1.0f - k.n) * (1.0f + k.n);
+template <bool GIVEN, int VC> __device__ __forceinline__ void slopes(const Coef<VC>& k, F<VC> hp, F<VC>& wg, F<VC>& wc) {
+  using V = F<VC>;
+  if (GIVEN) { wg = hp; wc = V::all(1.0f); return; }
+  wg = (k.q * k.e) * fma_(hp, V::all(-1.0f), k.n);
+  wc = k.q * (fma_(k.n, V::all(-1.0f), V::all(1.0f)) * (k.n + V::all(1.0f)));
 }
 
-// VC consecutive elements of a row
-template <class T, int VC> struct Vec;
-template <class T> struct Vec<T, 1> { T x; __device__ __forceinline__ float get(int) const { return to_f32(x); } __device__ __forceinline__ void set(int, float v) { x = from_f32<T>(v); } };
-template <> struct alignas(8) Vec<float, 2> { float x, y; __device__ __forceinline__ float get(int i) const { return i ? y : x; } __device__ __forceinline__ void set(int i, float v) { (i ? y : x) = v; } };
-template <> struct alignas(4) Vec<__nv_bfloat16, 2> {
-  __nv_bfloat162 v;
-  __device__ __forceinline__ float get(int i) const { return i ? __high2float(v) : __low2float(v); }
-  __device__ __forceinline__ void set(int i, float f) { (i ? v.y : v.x) = __float2bfloat16_rn(f); }
-};
-template <> struct alignas(4) Vec<__half, 2> {
-  __half2 v;
-  __device__ __forceinline__ float get(int i) const { return i ? __high2float(v) : __low2float(v); }
-  __device__ __forceinline__ void set(int i, float f) { (i ? v.y : v.x) = __float2half_rn(f); }
-};
-template <class T, int VC> __device__ __forceinline__ Vec<T, VC> load(const T* p) { return *reinterpret_cast<const Vec<T, VC>*>(p); }
-template <class T, int VC> __device__ __forceinline__ void store(T* p, const Vec<T, VC>& v) { *reinterpret_cast<Vec<T, VC>*>(p) = v; }
-template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
-  Vec<T, VC> v;
+template <int VC> __device__ __forceinline__ F<VC> load_state(const float* p, unsigned col) {
+  F<VC> f;
 #pragma unroll
-  for (int i = 0; i < VC; ++i) v.set(i, 0.f);
-  return v;
+  for (int v = 0; v < VC; ++v) f.at(v) = p ? p[col + v] : 0.f;
+  return f;
+}
+template <int VC> __device__ __forceinline__ void store_state(float* p, unsigned col, F<VC> f) {
+#pragma unroll
+  for (int v = 0; v < VC; ++v) p[col + v] = f.at(v);
 }
 
-// What a thread knows of its columns: first column, sequence, addresses of step 0
+// What a thread knows of its columns: the first one, its sequence and unit, the steps of that sequence
 template <class T> struct Column {
-  i64 col; int b, u, len;
+  unsigned col, b, u;
+  int len;
   bool live;
-  __device__ __forceinline__ Column(const ScanArgs& a, i64 c) : col(c) {
-    live = c < (i64)a.B * a.H;
-    b = live ? (int)(c / a.H) : 0;
-    u = live ? (int)(c - (i64)b * a.H) : 0;
+  __device__ __forceinline__ Column(const ScanArgs& a, unsigned c) : col(c) {
+    live = c < (unsigned)a.B * (unsigned)a.H;
+    b = live ? c / (unsigned)a.H : 0u;
+    u = live ? c - b * (unsigned)a.H : 0u;
     len = !live ? 0 : a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
   }
   __device__ __forceinline__ T* at(const ScanRows& r, int t) const { return reinterpret_cast<T*>(r.p) + (i64)t * r.ts + (i64)b * r.bs + u; }
   __device__ __forceinline__ bool fresh(const ScanArgs& a, int t) const {
-    return a.reset.p && reinterpret_cast<const uint8_t*>(a.reset.p)[(i64)t * a.reset.ts + (i64)b * a.reset.bs] != 0;
+    return reinterpret_cast<const uint8_t*>(a.reset.p)[(i64)t * a.reset.ts + (i64)b * a.reset.bs] != 0;
   }
 };
 
-template <class T, int CELL, int VC, bool BACK>
+template <class T, bool GIVEN, int VC, bool BACK>
 __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArgs a) {
-  constexpr bool FAST = sizeof(T) == 2;
-  const Column<T> q(a, ((i64)blockIdx.x * kShortThreads + threadIdx.x) * VC);
+  using V = F<VC>;
+  const Column<T> q(a, (blockIdx.x * kShortThreads + threadIdx.x) * VC);
   if (!q.live) return;
-  const float* first = BACK ? a.dhT : a.h0;
-  float h[VC];
-#pragma unroll
-  for (int v = 0; v < VC; ++v) h[v] = first ? first[q.col + v] : 0.f;
+  V h = load_state<VC>(BACK ? a.dhT : a.h0, q.col);
   for (int i = 0; i < a.T; ++i) {
     const int t = BACK ? a.T - 1 - i : i;
     if (t >= q.len) {
-      if (BACK) {
-        store<T, VC>(q.at(a.dgate, t), zeros<T, VC>());
-        store<T, VC>(q.at(a.dcand, t), zeros<T, VC>());
-      } else {
-        store<T, VC>(q.at(a.h, t), zeros<T, VC>());
-      }
+      store<T, VC>(q.at(BACK ? a.dgate : a.h, t), V::all(0.f));
+      if (BACK) store<T, VC>(q.at(a.dcand, t), V::all(0.f));
       continue;
     }
-    const bool fresh = q.fresh(a, t);
-    const Vec<T, VC> g = load<T, VC>(q.at(a.gate, t)), c = load<T, VC>(q.at(a.cand, t));
+    const bool fresh = a.reset.p && q.fresh(a, t);
+    const Coef<VC> k = coefficients<GIVEN, T, VC>(load<T, VC>(q.at(a.gate, t)), load<T, VC>(q.at(a.cand, t)), a);
     if (BACK) {
-      Vec<T, VC> hv = zeros<T, VC>(), sd = zeros<T, VC>(), dg, dc;
-      if (t > 0 && !fresh) hv = load<T, VC>(q.at(a.h, t - 1));
-      if (a.seed.p) sd = load<T, VC>(q.at(a.seed, t));
-#pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        const Coef k = coefficients<CELL, FAST>(g.get(v), c.get(v), a.dt);
-        const float hp = t == 0 && !fresh && a.h0 ? a.h0[q.col + v] : hv.get(v), lam = h[v] + sd.get(v);
-        float wg, wc;
-        slopes<CELL>(k, hp, a.dt, wg, wc);
-        dg.set(v, lam * wg);
-        dc.set(v, lam * wc);
-        h[v] = fresh ? 0.f : k.a * lam;
-      }
-      store<T, VC>(q.at(a.dgate, t), dg);
-      store<T, VC>(q.at(a.dcand, t), dc);
+      const V hp = fresh ? V::all(0.f) : t > 0 ? load<T, VC>(q.at(a.h, t - 1)).get() : load_state<VC>(a.h0, q.col);
+      const V lam = a.seed.p ? h + load<T, VC>(q.at(a.seed, t)).get() : h;
+      V wg, wc;
+      slopes<GIVEN, VC>(k, hp, wg, wc);
+      store<T, VC>(q.at(a.dgate, t), lam * wg);
+      store<T, VC>(q.at(a.dcand, t), lam * wc);
+      h = fresh ? V::all(0.f) : k.a * lam;
     } else {
-      Vec<T, VC> out;
-#pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        const Coef k = coefficients<CELL, FAST>(g.get(v), c.get(v), a.dt);
-        h[v] = fresh ? k.b : fmaf(k.a, h[v], k.b);
-        out.set(v, h[v]);
-      }
-      store<T, VC>(q.at(a.h, t), out);
+      h = fresh ? k.b : fma_(k.a, h, k.b);
+      store<T, VC>(q.at(a.h, t), h);
     }
   }
   float* last = BACK ? a.dh0 : a.hT;
-  if (last) {
-#pragma unroll
-    for (int v = 0; v < VC; ++v) last[q.col + v] = h[v];
-  }
+  if (last) store_state<VC>(last, q.col, h);
 }
 
-__device__ __forceinline__ int ld_acquire(const int* p) { int v; asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v; }
-__device__ __forceinline__ void st_release(int* p, int v) { asm volatile("st.release.gpu.global.s32 [%0], %1;" :: "l"(p), "r"(v) : "memory"); }
+// ---- words that tiles publish --------------------------------------------------------------------------------------------------
+
+constexpr unsigned kNone = 0xffffffffu;        // a NaN that no result is: NaN is published as 0x7fc00000
+__device__ __forceinline__ unsigned word_of(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
+__device__ __forceinline__ unsigned ld_word(const float* p) { unsigned v; asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v; }
+__device__ __forceinline__ void st_word(float* p, unsigned v) { asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" :: "l"(p), "r"(v) : "memory"); }
+__device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
+  unsigned long long v;
+  asm volatile("ld.relaxed.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+__device__ __forceinline__ void st_pair(unsigned long long* p, float2 v) {
+  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | word_of(v.x);
+  asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" :: "l"(p), "l"(w) : "memory");
+}
 __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t)); return t; }
 
-// h through the pair p.  A = 0 cuts what came before off, whatever it was (a reset sets it; 0 x NaN would not be 0).
-__device__ __forceinline__ float through(float2 p, float h) { return p.x == 0.f ? p.y : fmaf(p.x, h, p.y); }
+// h through the pair p.  cut (some sequence starts anew somewhere): A = 0 cuts off what came before, whatever it was (0 x NaN would not).
+__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && p.x == 0.f ? p.y : fmaf(p.x, h, p.y); }
+__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(cut && p.x == 0.f ? 0.f : p.x * q.x, through(p, q.y, cut)); }
 
-// The state in front of tile k of column tile c, for the warp's columns: waits until a state and all pairs after it have been published.
-template <int VC> __device__ __forceinline__ void look_back(const ScanArgs& a, int k, int c, int lane, float (&h)[VC]) {
-  int from = -1;                               // the tile whose state is taken
-  uint64_t t0 = 0;
-  for (unsigned round = 0; from < 0; ++round) {
-    int last = k - 1;                          // tiles last, last - 1, ... of this look
-#pragma unroll 1
-    for (int w = 0; w < kLook && last >= 0; ++w, last -= 32) {
-      const int f = last - lane >= 0 ? ld_acquire(a.flags + (i64)(last - lane) * a.nc + c) : 0;
-      const unsigned state = __ballot_sync(0xffffffffu, f == 2), none = __ballot_sync(0xffffffffu, f == 0);
-      const int s = state ? __ffs(state) - 1 : 32, n = none ? __ffs(none) - 1 : 32;
-      if (s < n) { from = last - s; break; }
-      if (n < 32) break;                       // a tile in between has not published anything yet
-    }
-    if (from < 0 && (round & 31u) == 31u) {
-      int stop = 0;
-      if (lane == 0) {
-        const uint64_t t = now_ns();
-        if (t0 == 0) t0 = t;
-        stop = *(volatile int*)a.status != 0;
-        if (!stop && t - t0 > kWaitNs) { atomicExch(a.status, 1); stop = 1; }
-      }
-      if (__shfl_sync(0xffffffffu, stop, 0)) {
-#pragma unroll
-        for (int v = 0; v < VC; ++v) h[v] = __int_as_float(0x7fc00000);      // the results are void, and look it
-        return;
-      }
-    }
+// One round of a wait, for the whole warp: true once it has run out, here or elsewhere (the status word says so).
+__device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, unsigned round, uint64_t& t0) {
+  if ((round & 31u) != 31u) return false;
+  int stop = 0;
+  if (lane == 0) {
+    const uint64_t t = now_ns();
+    if (t0 == 0) t0 = t;
+    stop = *(volatile int*)a.status != 0;
+    if (!stop && t - t0 > kWaitNs) { atomicExch(a.status, 1); stop = 1; }
   }
-  __syncwarp();                                // what one lane acquired is ordered in front of every lane's loads
-  const i64 row = (i64)a.nc * (32 * VC), col = (i64)c * (32 * VC) + lane * VC;
-#pragma unroll
-  for (int v = 0; v < VC; ++v) h[v] = __ldcg(a.states + from * row + col + v);
-  const float2* p = a.pairs + (from + 1) * row + col;
-#pragma unroll 4
-  for (int j = from + 1; j < k; ++j, p += row) {
-#pragma unroll
-    for (int v = 0; v < VC; ++v) h[v] = through(__ldcg(p + v), h[v]);
-  }
+  return __shfl_sync(0xffffffffu, stop, 0) != 0;
 }
 
-template <class T, int CELL, int VC, bool BACK>
-__global__ void __launch_bounds__(kWarps * 32) scan_tile_kernel(const ScanArgs a) {
-  constexpr bool FAST = sizeof(T) == 2;
-  constexpr int S = kSteps, CT = 32 * VC;
-  __shared__ float2 pair[kWarps][CT];
-  __shared__ float front[CT];
-  __shared__ unsigned tile_s;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  unsigned tile = blockIdx.x;
-  if (a.nk > 1) {
-    if (threadIdx.x == 0) tile_s = atomicAdd(a.ticket, 1u);
-    __syncthreads();
-    tile = tile_s;
+// The state in front of tile k of column tile c, for the warp's columns: carried from the last published state through the pairs after
+// it.  Words of a tile are published together, so one of them (the first column's) tells the lanes how far back to go.  A tile that found
+// the state in front of it at once publishes no pair, only its state: whoever misses a word looks again from the start.
+template <int VC> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, int c, int lane) {
+  const i64 row = (i64)a.nc * (32 * VC), col = (i64)c * (32 * VC);
+  uint64_t t0 = 0;
+  for (unsigned round = 0; !waited_too_long(a, lane, round, t0); ++round) {
+    int from = -1;                             // the tile whose state is taken
+    int last = k - 1;
+#pragma unroll 1
+    for (int w = 0; w < kLook && last >= 0 && from < 0; ++w, last -= 32) {
+      const bool there = last - lane >= 0 && ld_word(a.states + (last - lane) * row + col) != kNone;
+      const unsigned m = __ballot_sync(0xffffffffu, there);
+      if (m) from = last - (__ffs(m) - 1);
+    }
+    if (from < 0) continue;
+    F<VC> h;
+    bool there = true;
+#pragma unroll
+    for (int v = 0; v < VC; ++v) {
+      const unsigned w = ld_word(a.states + from * row + col + lane * VC + v);
+      there = there && w != kNone;
+      h.at(v) = __uint_as_float(w);
+    }
+#pragma unroll 1
+    for (int j = from + 1; j < k && there; j += kPairs) {
+      float2 p[kPairs][VC];
+      const int n = min(kPairs, k - j);
+      const unsigned long long* at = a.pairs + j * row + col + lane * VC;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i)
+#pragma unroll
+        for (int v = 0; v < VC; ++v) p[i][v] = i < n ? ld_pair(at + i * row + v) : make_float2(1.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i)
+#pragma unroll
+        for (int v = 0; v < VC; ++v)
+          if (i < n) {
+            there = there && __float_as_uint(p[i][v].x) != kNone;
+            h.at(v) = through(p[i][v], h.at(v), a.reset.p != nullptr);
+          }
+    }
+    if (__all_sync(0xffffffffu, there)) return h;
   }
-  const int k = (int)(tile / (unsigned)a.nc), c = (int)(tile - (unsigned)k * (unsigned)a.nc);
-  const Column<T> q(a, (i64)c * CT + lane * VC);
-  const int i0 = k * kTileSteps + warp * S;    // the thread's first step, counted from the scan's start
+  return F<VC>::all(__uint_as_float(0x7fc00000u));      // the results are void, and look it
+}
+
+// A tile's place, worked out by one thread for the block
+struct alignas(16) Place { int k, c; unsigned b, u; };      // chunk of time (-1: no tile), column tile; sequence and unit of its first column
+__device__ __forceinline__ Place place_of(const ScanArgs& a, unsigned tile, int columns) {
+  Place p;
+  if (tile >= (unsigned)a.nk * (unsigned)a.nc) return Place{-1, 0, 0u, 0u};
+  p.k = (int)(tile / (unsigned)a.nc);
+  p.c = (int)(tile - (unsigned)p.k * (unsigned)a.nc);
+  const unsigned col = (unsigned)p.c * (unsigned)columns;
+  p.b = col / (unsigned)a.H;
+  p.u = col - p.b * (unsigned)a.H;
+  return p;
+}
+
+template <class T, bool GIVEN, int VC, bool BACK>
+__global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
+  constexpr bool STAGED = VC * sizeof(T) == 8;
+  constexpr int S = kStepsOf<VC, BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
+  extern __shared__ __align__(16) char stage[];      // [tiles ahead][ARRAYS][S][threads] words of 8 bytes
+  constexpr unsigned ALL = (1u << S) - 1u;
+  using V = F<VC>;
+  __shared__ __align__(16) float2 pair[2][kWarps][CT];
+  constexpr int D = STAGED ? kAhead : 1, RING = 4;
+  static_assert(D < RING - 1, "a place is written while the one before it and those ahead are in use");
+  __shared__ Place place[RING];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const i64 row = (i64)a.nc * CT;
+  const bool cut = a.reset.p != nullptr;
   const auto time_of = [&](int i) { return BACK ? a.T - 1 - i : i; };
 
-  // the thread's steps: read once, kept as coefficients (and what the gradients need)
-  float ca[S][VC], cb[S][VC], wg[BACK ? S : 1][VC], wc[BACK ? S : 1][VC];      // cb: b, backward: the seed
-  unsigned inside = 0, fresh = 0;
-  {
-    Vec<T, VC> g[S], n[S], hv[BACK ? S : 1], sd[BACK ? S : 1];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int t = time_of(i0 + s);
-      const bool in = t >= 0 && t < q.len;
-      g[s] = n[s] = zeros<T, VC>();
-      if (BACK) hv[BACK ? s : 0] = sd[BACK ? s : 0] = zeros<T, VC>();
-      if (in) {
-        inside |= 1u << s;
-        g[s] = load<T, VC>(q.at(a.gate, t));
-        n[s] = load<T, VC>(q.at(a.cand, t));
-        if (BACK) {
-          if (t > 0) hv[BACK ? s : 0] = load<T, VC>(q.at(a.h, t - 1));
-          if (a.seed.p) sd[BACK ? s : 0] = load<T, VC>(q.at(a.seed, t));
-        }
-      }
+  // where the thread stands in a tile: sequence and unit of its columns, its first step counted from the scan's start
+  struct Spot { unsigned b, u; int i0; bool live; };
+  const auto spot_of = [&](const Place& p) {
+    Spot s;
+    s.b = p.b;
+    s.u = p.u + lane * VC;
+    if (s.u >= (unsigned)a.H) {                // the tile reaches into the next sequences
+      const unsigned n = s.u / (unsigned)a.H;
+      s.b += n;
+      s.u -= n * (unsigned)a.H;
     }
-    if (a.reset.p) {
-#pragma unroll
-      for (int s = 0; s < S; ++s)
-        if ((inside >> s & 1u) && q.fresh(a, time_of(i0 + s))) fresh |= 1u << s;
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const bool in = inside >> s & 1u, fr = fresh >> s & 1u;
-#pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        const Coef o = coefficients<CELL, FAST>(g[s].get(v), n[s].get(v), a.dt);
-        ca[s][v] = !in ? 1.f : fr ? 0.f : o.a;
-        if (BACK) {
-          float hp = hv[BACK ? s : 0].get(v);
-          if (time_of(i0 + s) == 0) hp = in && a.h0 ? a.h0[q.col + v] : 0.f;
-          if (fr) hp = 0.f;
-          cb[s][v] = sd[BACK ? s : 0].get(v);
-          slopes<CELL>(o, hp, a.dt, wg[BACK ? s : 0][v], wc[BACK ? s : 0][v]);
-        } else {
-          cb[s][v] = in ? o.b : 0.f;
-        }
-      }
-    }
-  }
-  // one step of the scan: forward h -> a h + b, backward mu -> a (mu + seed)
-  const auto step = [&](int s, int v, float h) {
-    if (fresh >> s & 1u) return BACK ? 0.f : cb[s][v];
-    return BACK ? ca[s][v] * (h + cb[s][v]) : fmaf(ca[s][v], h, cb[s][v]);
+    s.i0 = p.k * TT + warp * S;
+    s.live = s.b < (unsigned)a.B;
+    return s;
   };
+  const auto at = [&](const ScanRows& r, const Spot& s, int t) { return reinterpret_cast<T*>(r.p) + ((i64)t * r.ts + (i64)s.b * r.bs + s.u); };
+
+  // The thread's own steps of a tile, as they come from memory.  Rows that allow it are staged in shared memory by asynchronous copies
+  // (a thread reads back what it copied itself, so nobody waits for anybody), which leaves the registers to the tile in work.
+  const unsigned slot0 = (unsigned)__cvta_generic_to_shared(stage) + threadIdx.x * 8u;
+  constexpr unsigned kSlot = kWarps * 32 * 8u, kTile = ARRAYS * S * kSlot;
+  Vec<T, VC> regs[STAGED ? 1 : ARRAYS][STAGED ? 1 : S];
+  const auto bring = [&](unsigned d, int array, int s, const T* p, bool in) {
+    if (STAGED) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(slot0 + d * kTile + (array * S + s) * kSlot), "l"(p), "r"(in ? 8 : 0) : "memory");
+    } else {
+      regs[STAGED ? 0 : array][STAGED ? 0 : s] = in ? load<T, VC>(p) : zeros<T, VC>();
+    }
+  };
+  const auto raw = [&](unsigned d, int array, int s) {
+    if (!STAGED) return regs[STAGED ? 0 : array][STAGED ? 0 : s];
+    return *reinterpret_cast<const Vec<T, VC>*>(stage + d * kTile + threadIdx.x * 8u + (array * S + s) * kSlot);
+  };
+  // -> which of the steps lie in the sequence, and (from bit 16 on) which of them start one
+  const auto fetch = [&](const Spot& s, unsigned d) {
+    unsigned inside, fresh;
+    const int len = !s.live ? 0 : a.lengths ? min(max(a.lengths[s.b], 0), a.T) : a.T;
+    // steps i0 .. i0 + S - 1 of the scan that lie in the sequence
+    const int lo = BACK ? max(0, a.T - len - s.i0) : 0, hi = BACK ? min(S, a.T - s.i0) : min(S, len - s.i0);
+    inside = hi > lo ? (ALL >> (S - hi)) & (ALL << lo) : 0u;
+    fresh = 0u;
+    const int t0 = time_of(s.i0);
+    const T *pg = at(a.gate, s, t0), *pc = at(a.cand, s, t0);
+    const T *ph = BACK ? at(a.h, s, t0 - 1) : nullptr, *ps = BACK ? at(a.seed, s, t0) : nullptr;
+    const i64 dg = BACK ? -a.gate.ts : a.gate.ts, dc = BACK ? -a.cand.ts : a.cand.ts;
+    const bool seeded = BACK && a.seed.p;
+    if (__all_sync(0xffffffffu, inside == ALL && !cut && (!BACK || (t0 >= S && seeded)))) {
 #pragma unroll
-  for (int v = 0; v < VC; ++v) {
-    float A = 1.f, h = 0.f;
+      for (int i = 0; i < S; ++i) {
+        bring(d, 0, i, pg + i * dg, true);
+        bring(d, 1, i, pc + i * dc, true);
+        if (BACK) {
+          bring(d, 2, i, ph - i * a.h.ts, true);
+          bring(d, 3, i, ps - i * a.seed.ts, true);
+        }
+      }
+    } else {
+      // (what is not inside is not read: the address of the array's first element stands in for it)
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        const bool in = inside >> i & 1u;
+        bring(d, 0, i, in ? pg + i * dg : reinterpret_cast<const T*>(a.gate.p), in);
+        bring(d, 1, i, in ? pc + i * dc : reinterpret_cast<const T*>(a.cand.p), in);
+        if (BACK) {
+          const bool before = in && t0 - i > 0, sd = in && seeded;
+          bring(d, 2, i, before ? ph - i * a.h.ts : reinterpret_cast<const T*>(a.h.p), before);
+          bring(d, 3, i, sd ? ps - i * a.seed.ts : reinterpret_cast<const T*>(a.gate.p), sd);
+        }
+        if (cut && in && reinterpret_cast<const uint8_t*>(a.reset.p)[(i64)time_of(s.i0 + i) * a.reset.ts + (i64)s.b * a.reset.bs]) fresh |= 1u << i;
+      }
+    }
+    if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory");
+    return inside | fresh << 16;
+  };
+
+  // Tiles are drawn from the counter (which starts at 2^32 - 1) by thread 32.  deep: D + 1 at the start, and from then on one round
+  // before a number is told to the others, so that nobody waits for it.  Otherwise (few tiles: they would all go to the first blocks)
+  // one at a time, and nothing is fetched ahead.
+  unsigned drawn = blockIdx.x - gridDim.x;
+  const auto draw = [&]() { return drawn = a.nk > 1 ? atomicAdd(a.ticket, 1u) + 1u : drawn + gridDim.x; };
+  const auto none = [&]() { if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory"); return 0u; };
+  unsigned ahead[D];                           // what fetch() said of the tiles to come
+#pragma unroll
+  for (int i = 0; i < D; ++i) ahead[i] = 0u;
+  if (a.deep) {
+    if (threadIdx.x == 32) {
+      for (int i = 0; i <= D; ++i) place[i] = place_of(a, draw(), CT);
+      draw();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const Place p = place[i];
+      ahead[i] = p.k >= 0 ? fetch(spot_of(p), i) : none();
+    }
+  }
+
+  // one tile; ODD: some step of the warp lies outside its sequence, starts a sequence or (backward) is the first one
+  const auto work = [&](auto odd_, unsigned d, unsigned turn, const Place& here, const Spot& now, unsigned in_now, unsigned fresh_now) {
+    constexpr bool ODD = decltype(odd_)::value;
+    const int k = here.k, c = here.c;
+    const unsigned buf = turn & 1u;
+    const i64 word = k * row + (i64)c * CT + lane * VC;
+    // the state that the tile before has published, asked for early: it is usually there
+    unsigned early[VC];
+    if (k > 0) {
+#pragma unroll
+      for (int v = 0; v < VC; ++v) early[v] = ld_word(a.states + word - row + v);
+    }
+    const unsigned told = drawn;
+    if (threadIdx.x == 32 && a.deep) draw();
+
+    V ca[S], cb[S], wg[SB], wc[SB];            // cb: b, backward: the seed
+    if (STAGED) asm volatile("cp.async.wait_group %0;" :: "n"(D - 1) : "memory");      // (all but the D - 1 last groups)
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      A = (fresh >> s & 1u) ? 0.f : ca[s][v] * A;
-      h = step(s, v, h);
+      const Coef<VC> o = coefficients<GIVEN, T, VC>(raw(d, 0, s), raw(d, 1, s), a);
+      ca[s] = o.a;
+      if (BACK) {
+        V hp = raw(d, 2, s).get();
+        if (ODD && time_of(now.i0 + s) == 0 && (in_now >> s & 1u)) hp = load_state<VC>(a.h0, now.b * (unsigned)a.H + now.u);
+        if (ODD && (fresh_now >> s & 1u)) hp = V::all(0.f);
+        cb[s] = raw(d, 3, s).get();
+        slopes<GIVEN, VC>(o, hp, wg[BACK ? s : 0], wc[BACK ? s : 0]);
+      } else {
+        cb[s] = o.b;
+      }
+      if (ODD) {
+        if (!(in_now >> s & 1u)) { ca[s] = V::all(1.f); cb[s] = V::all(0.f); }
+        if (fresh_now >> s & 1u) ca[s] = V::all(0.f);
+      }
     }
-    pair[warp][lane * VC + v] = make_float2(A, h);
-  }
-  __syncthreads();
+    unsigned theirs = 0u;
+    if (a.deep) {
+      const Place later = place[(turn + D) % RING];
+      theirs = later.k >= 0 ? fetch(spot_of(later), d) : none();
+    }
 
-  if (warp == 0) {
-    float2 whole[VC];
-    float h[VC];
+    // one step of the scan: forward h -> a h + b, backward mu -> a (mu + seed)
+    const auto step = [&](int s, V h) {
+      if (ODD && (fresh_now >> s & 1u)) return BACK ? V::all(0.f) : cb[s];
+      return BACK ? ca[s] * (h + cb[s]) : fma_(ca[s], h, cb[s]);
+    };
+    V A = V::all(1.f), h = V::all(0.f);
 #pragma unroll
-    for (int v = 0; v < VC; ++v) {
-      whole[v] = pair[0][lane * VC + v];
+    for (int s = 0; s < S; ++s) {
+      A = ODD && (fresh_now >> s & 1u) ? V::all(0.f) : s == 0 ? ca[s] : ca[s] * A;
+      h = step(s, h);
+    }
+#pragma unroll
+    for (int v = 0; v < VC; ++v) pair[buf][warp][lane * VC + v] = make_float2(A.at(v), h.at(v));
+    if (threadIdx.x == 32 && a.deep) place[(turn + D + 1) % RING] = place_of(a, told, CT);
+    __syncthreads();                           // the only meeting of the block's warps: the arrays are used in turn
+
+    // every warp carries the state in front of the tile through the pairs of the warps before it; the last one speaks for the tile
+    const bool speaker = warp == kWarps - 1 && k + 1 < a.nk;
+    float2 whole[VC];
+    if (speaker) {
+#pragma unroll
+      for (int v = 0; v < VC; ++v) whole[v] = pair[buf][0][lane * VC + v];
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) {
-        const float2 p = pair[w][lane * VC + v];
-        whole[v] = make_float2(p.x == 0.f ? 0.f : p.x * whole[v].x, through(p, whole[v].y));
+#pragma unroll
+        for (int v = 0; v < VC; ++v) whole[v] = through(pair[buf][w][lane * VC + v], whole[v], cut);
       }
     }
-    const bool more = k + 1 < a.nk;
-    const i64 at = ((i64)k * a.nc + c) * CT + lane * VC;
-    int* flag = a.flags + (i64)k * a.nc + c;
     if (k == 0) {
       const float* first = BACK ? a.dhT : a.h0;
-#pragma unroll
-      for (int v = 0; v < VC; ++v) h[v] = q.live && first ? first[q.col + v] : 0.f;
+      h = now.live ? load_state<VC>(first, now.b * (unsigned)a.H + now.u) : V::all(0.f);
     } else {
-      if (more) {
+      bool known = true;
 #pragma unroll
-        for (int v = 0; v < VC; ++v) __stcg(a.pairs + at + v, whole[v]);
-        __syncwarp();
-        if (lane == 0) { __threadfence(); st_release(flag, 1); }
+      for (int v = 0; v < VC; ++v) {
+        known = known && early[v] != kNone;
+        h.at(v) = __uint_as_float(early[v]);
       }
-      look_back<VC>(a, k, c, lane, h);
-    }
-    if (more) {
+      if (!__all_sync(0xffffffffu, known)) {
+        if (speaker) {
 #pragma unroll
-      for (int v = 0; v < VC; ++v) __stcg(a.states + at + v, through(whole[v], h[v]));
-      __syncwarp();
-      if (lane == 0) { __threadfence(); st_release(flag, 2); }
-    }
-#pragma unroll
-    for (int v = 0; v < VC; ++v) front[lane * VC + v] = h[v];
-  }
-  __syncthreads();
-
-  float h[VC];
-#pragma unroll
-  for (int v = 0; v < VC; ++v) {
-    h[v] = front[lane * VC + v];
-    for (int w = 0; w < warp; ++w) h[v] = through(pair[w][lane * VC + v], h[v]);
-  }
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    const int t = time_of(i0 + s);
-    const bool in = inside >> s & 1u, write = q.live && t >= 0 && t < a.T;
-    Vec<T, VC> x = zeros<T, VC>(), y = zeros<T, VC>();
-#pragma unroll
-    for (int v = 0; v < VC; ++v) {
-      if (BACK) {
-        const float lam = h[v] + cb[s][v];
-        if (in) {
-          x.set(v, lam * wg[BACK ? s : 0][v]);
-          y.set(v, lam * wc[BACK ? s : 0][v]);
+          for (int v = 0; v < VC; ++v) st_pair(a.pairs + word + v, whole[v]);
         }
+        h = look_back<VC>(a, k, c, lane);
       }
-      h[v] = step(s, v, h[v]);
-      if (!BACK && in) x.set(v, h[v]);
     }
-    if (write) {
-      store<T, VC>(q.at(BACK ? a.dgate : a.h, t), x);
-      if (BACK) store<T, VC>(q.at(a.dcand, t), y);
-    }
-  }
-  float* last = BACK ? a.dh0 : a.hT;
-  if (last && k + 1 == a.nk && warp == kWarps - 1 && q.live) {
+    if (speaker) {
 #pragma unroll
-    for (int v = 0; v < VC; ++v) last[q.col + v] = h[v];
+      for (int v = 0; v < VC; ++v) st_word(a.states + word + v, word_of(through(whole[v], h.at(v), cut)));
+    }
+#pragma unroll
+    for (int w = 0; w < kWarps - 1; ++w) {
+      if (w < warp) {
+#pragma unroll
+        for (int v = 0; v < VC; ++v) h.at(v) = through(pair[buf][w][lane * VC + v], h.at(v), cut);
+      }
+    }
+    T *po = at(BACK ? a.dgate : a.h, now, time_of(now.i0)), *pw = BACK ? at(a.dcand, now, time_of(now.i0)) : nullptr;
+    const i64 dout = BACK ? -a.dgate.ts : a.h.ts;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      V x, y;
+      if (BACK) {
+        const V lam = h + cb[s];
+        x = lam * wg[BACK ? s : 0];
+        y = lam * wc[BACK ? s : 0];
+      }
+      h = step(s, h);
+      if (!BACK) x = h;
+      bool write = true;
+      if (ODD) {
+        const int t = time_of(now.i0 + s);
+        write = now.live && t >= 0 && t < a.T;
+        if (!(in_now >> s & 1u)) x = y = V::all(0.f);
+      }
+      if (write) {
+        store<T, VC>(po + s * dout, x);
+        if (BACK) store<T, VC>(pw - s * a.dcand.ts, y);
+      }
+    }
+    float* last = BACK ? a.dh0 : a.hT;
+    if (last && k + 1 == a.nk && warp == kWarps - 1 && now.live) store_state<VC>(last, now.b * (unsigned)a.H + now.u, h);
+    return theirs;
+  };
+  for (unsigned turn = 0, d = 0;; ++turn, d = d + 1 == D ? 0 : d + 1) {
+    if (!a.deep) {
+      if (threadIdx.x == 32) place[turn % RING] = place_of(a, draw(), CT);
+      __syncthreads();
+    }
+    const Place here = place[turn % RING];
+    if (here.k < 0) break;
+    const Spot now = spot_of(here);
+    if (!a.deep) {
+      ahead[0] = fetch(now, d);
+#pragma unroll
+      for (int i = 1; i < D; ++i) none();
+    }
+    const unsigned bits = ahead[0];
+    unsigned theirs;
+    if (__all_sync(0xffffffffu, bits == ALL && !(BACK && time_of(now.i0 + S - 1) <= 0)))
+      theirs = work(std::false_type{}, d, turn, here, now, bits & 0xffffu, bits >> 16);
+    else
+      theirs = work(std::true_type{}, d, turn, here, now, bits & 0xffffu, bits >> 16);
+#pragma unroll
+    for (int i = 0; i + 1 < D; ++i) ahead[i] = ahead[i + 1];
+    ahead[D - 1] = theirs;
   }
 }
 
@@ -410,6 +659,8 @@ int check_scan(const gated_scan_args* x, bool back, ScanArgs& a) {
   if (!scan_sizes_served(x->T, x->B, x->H)) return MGRIT_UNSUPPORTED;
   a = ScanArgs{};
   a.T = x->T; a.B = x->B; a.H = x->H; a.dt = x->dt;
+  a.K = x->cell == MGRIT_CELL_IMPLICIT ? 1.0f + x->dt : 1.0f;
+  a.L = x->cell == MGRIT_CELL_IMPLICIT ? 1.0f : 1.0f - x->dt;
   a.h0 = x->h0; a.lengths = x->lengths;
   if (!aligned4(x->h0) || !aligned4(x->lengths)) return MGRIT_INVALID_ARG;
   if (back) {
@@ -441,15 +692,15 @@ int copy_state(float* dst, const float* src, size_t n, cudaStream_t s) {
   return e == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
-// Workspace: counter | flags | pairs | states, for the narrower of the column tiles (which has more flags and as many values)
-struct ScanSpace { size_t flags, pairs, states, total; };
-ScanSpace scan_space(int T, i64 cols) {
-  const size_t up = 255, nk = ((size_t)T + kTileSteps - 1) / kTileSteps, padded = ((size_t)cols + 63) / 64 * 64;
+// Workspace: counter | states | pairs, filled with kNone.  Columns are padded to the wider column tile, time to the shortest one.
+constexpr int kLeastSteps = kStepsOf<2, true> * kWarps;
+static_assert(kLeastSteps <= kStepsOf<2, false> * kWarps && kLeastSteps <= kStepsOf<1, true> * kWarps, "the shortest tile sizes the workspace");
+struct ScanSpace { size_t states, pairs, total; };
+ScanSpace scan_space(i64 nk, i64 padded) {
   ScanSpace s;
-  s.flags = 256;
-  s.pairs = (s.flags + nk * (padded / 32) * sizeof(int) + up) & ~up;
-  s.states = s.pairs + nk * padded * sizeof(float2);
-  s.total = (s.states + nk * padded * sizeof(float) + up) & ~up;
+  s.states = 256;
+  s.pairs = s.states + (((size_t)nk * padded * sizeof(float) + 255) & ~(size_t)255);
+  s.total = s.pairs + (((size_t)nk * padded * sizeof(float2) + 255) & ~(size_t)255);
   return s;
 }
 
@@ -464,56 +715,77 @@ int* scan_status_ptr() {
   return g_scan_status_ptrs[dev];
 }
 
-// two columns a thread where rows allow it: H even, all strides even and all addresses on pairs
-bool pairs_of_columns(const ScanArgs& a, int dtype) {
-  const uintptr_t mask = 2 * elem_size(dtype) - 1;
-  const auto fits = [&](const ScanRows& r) { return !r.p || (((uintptr_t)r.p & mask) == 0 && r.ts % 2 == 0 && r.bs % 2 == 0); };
-  return a.H % 2 == 0 && fits(a.gate) && fits(a.cand) && fits(a.h) && fits(a.seed) && fits(a.dgate) && fits(a.dcand);
+// several columns a thread where rows allow it: units and strides whole words of 8 bytes, all addresses on such words
+bool wide_columns(const ScanArgs& a, int dtype) {
+  const int n = 8 / (int)elem_size(dtype);
+  const auto fits = [&](const ScanRows& r) { return !r.p || (((uintptr_t)r.p & 7u) == 0 && r.ts % n == 0 && r.bs % n == 0); };
+  return a.H % n == 0 && fits(a.gate) && fits(a.cand) && fits(a.h) && fits(a.seed) && fits(a.dgate) && fits(a.dcand);
 }
 
-template <class T, int CELL, int VC, bool BACK> cudaError_t launch_scan(const ScanArgs& a, cudaStream_t s) {
+// blocks of a kernel that fit the device at once, asked once for each kernel and device
+template <class K> int resident_blocks(K kern, int threads, int smem, int (&known)[kMaxDevices]) {
+  const int dev = current_device_slot();
+  if (dev < 0) return 0;
+  if (!known[dev]) {
+    int per_sm = 0, sms = 0;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, smem) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return 0;
+    known[dev] = per_sm * sms;
+  }
+  return known[dev];
+}
+
+template <class T, bool GIVEN, int VC, bool BACK> int launch_scan(ScanArgs& a, void* ws, size_t ws_bytes, cudaStream_t s) {
   const i64 cols = (i64)a.B * a.H;
   if (a.T <= kShort) {
-    scan_short_kernel<T, CELL, VC, BACK><<<(unsigned)((cols / VC + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
+    scan_short_kernel<T, GIVEN, VC, BACK><<<(unsigned)((cols / VC + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
   } else {
-    scan_tile_kernel<T, CELL, VC, BACK><<<(unsigned)a.nk * (unsigned)a.nc, kWarps * 32, 0, s>>>(a);
+    constexpr int steps = kStepsOf<VC, BACK> * kWarps;
+    const i64 nc = (cols + 32 * VC - 1) / (32 * VC), nk = ((i64)a.T + steps - 1) / steps;
+    if (nk * nc >= INT32_MAX) return MGRIT_UNSUPPORTED;
+    a.nk = (int)nk; a.nc = (int)nc;
+    if (nk > 1) {
+      const ScanSpace sp = scan_space(nk, nc * 32 * VC);
+      if (!ws || ((uintptr_t)ws & 255u)) return MGRIT_INVALID_ARG;
+      if (ws_bytes < sp.total) return MGRIT_WORKSPACE_TOO_SMALL;
+      char* w = static_cast<char*>(ws);
+      a.ticket = reinterpret_cast<unsigned*>(w);
+      a.states = reinterpret_cast<float*>(w + sp.states);
+      a.pairs = reinterpret_cast<unsigned long long*>(w + sp.pairs);
+      a.status = scan_status_ptr();
+      if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
+    }
+    static int known[kMaxDevices];
+    constexpr int smem = VC * sizeof(T) == 8 ? kAhead * (BACK ? 4 : 2) * kStepsOf<VC, BACK> * kWarps * 32 * 8 : 0;
+    const int most = resident_blocks(scan_tile_kernel<T, GIVEN, VC, BACK>, kWarps * 32, smem, known);
+    if (most <= 0) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
+    // every block gets four tiles or more: enough that the first ones to run may take several at once
+    a.deep = nk * nc >= 4 * (i64)most;
+    scan_tile_kernel<T, GIVEN, VC, BACK><<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
   }
   count_launch();
-  return cudaGetLastError();
-}
-template <class T, int CELL> cudaError_t launch_scan(const ScanArgs& a, int vc, bool back, cudaStream_t s) {
-  if (vc == 2) return back ? launch_scan<T, CELL, 2, true>(a, s) : launch_scan<T, CELL, 2, false>(a, s);
-  return back ? launch_scan<T, CELL, 1, true>(a, s) : launch_scan<T, CELL, 1, false>(a, s);
+  return cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
 int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cudaStream_t s) {
   ScanArgs a;
-  const int rc = check_scan(x, back, a);
+  int rc = check_scan(x, back, a);
   if (rc != MGRIT_OK) return rc;
   if (a.T == 0 || a.B == 0) return back ? copy_state(a.dh0, a.dhT, (size_t)a.B * a.H, s) : copy_state(a.hT, a.h0, (size_t)a.B * a.H, s);
-  const int vc = pairs_of_columns(a, x->dtype) ? 2 : 1;
-  const i64 cols = (i64)a.B * a.H, nc = (cols + 32 * vc - 1) / (32 * vc), nk = ((i64)a.T + kTileSteps - 1) / kTileSteps;
-  if (nk * nc >= INT32_MAX) return MGRIT_UNSUPPORTED;
-  a.nk = (int)nk; a.nc = (int)nc;
-  if (nk > 1) {
-    const ScanSpace sp = scan_space(a.T, cols);
-    if (!ws || ((uintptr_t)ws & 255u)) return MGRIT_INVALID_ARG;
-    if (ws_bytes < sp.total) return MGRIT_WORKSPACE_TOO_SMALL;
-    char* w = static_cast<char*>(ws);
-    a.ticket = reinterpret_cast<unsigned*>(w);
-    a.flags = reinterpret_cast<int*>(w + sp.flags);
-    a.pairs = reinterpret_cast<float2*>(w + sp.pairs);
-    a.states = reinterpret_cast<float*>(w + sp.states);
-    a.status = scan_status_ptr();
-    if (!a.status || cudaMemsetAsync(ws, 0, sp.flags + (size_t)(nk * nc) * sizeof(int), s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
-  }
-  cudaError_t e = cudaSuccess;
+  const bool wide = wide_columns(a, x->dtype), given = x->cell == MGRIT_SCAN_COEFFICIENTS;
   with_elem(x->dtype, [&](auto tag) {
     using T = decltype(tag);
-    e = x->cell == MGRIT_CELL_CLASSIC ? launch_scan<T, MGRIT_CELL_CLASSIC>(a, vc, back, s)
-      : x->cell == MGRIT_CELL_IMPLICIT ? launch_scan<T, MGRIT_CELL_IMPLICIT>(a, vc, back, s) : launch_scan<T, MGRIT_SCAN_COEFFICIENTS>(a, vc, back, s);
+    const auto pick = [&](auto g) {
+      constexpr bool G = decltype(g)::value;
+      constexpr int W = kWide<T>;
+      rc = wide ? (back ? launch_scan<T, G, W, true>(a, ws, ws_bytes, s) : launch_scan<T, G, W, false>(a, ws, ws_bytes, s))
+               : (back ? launch_scan<T, G, 1, true>(a, ws, ws_bytes, s) : launch_scan<T, G, 1, false>(a, ws, ws_bytes, s));
+    };
+    if (given) pick(std::true_type{}); else pick(std::false_type{});
   });
-  return e == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
+  return rc;
 }
 
 }  // namespace
@@ -537,8 +809,8 @@ int scan_clear_device_status() {
 extern "C" {
 
 size_t gated_scan_workspace_bytes(int32_t T, int32_t B, int32_t H) {
-  if (!mg::scan_sizes_served(T, B, H) || T <= mg::kTileSteps || B == 0) return 0;
-  return mg::scan_space(T, (mg::i64)B * H).total;
+  if (!mg::scan_sizes_served(T, B, H) || T <= mg::kLeastSteps || B == 0) return 0;
+  return mg::scan_space(((mg::i64)T + mg::kLeastSteps - 1) / mg::kLeastSteps, ((mg::i64)B * H + 127) / 128 * 128).total;
 }
 
 int gated_scan_forward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream) {
