@@ -29,7 +29,7 @@ int* g_scan_status_ptrs[kMaxDevices] = {nullptr};
 
 struct ScanRows { char* p; i64 ts, bs; };      // strides in elements
 struct ScanArgs {
-  int T, B, H;
+  int T, B, H, Hp;                             // Hp: H rounded up to whole threads (tile kernel)
   float dt, K, L;                              // gate: q = dt / (K + E), a = (L + E) / (K + E); see coefficients()
   ScanRows gate, cand, h, seed, dgate, dcand, reset;
   const float* h0; const int32_t* lengths; float* hT;
@@ -44,9 +44,6 @@ constexpr int kShortThreads = 128;
 #ifndef SCAN_W
 #define SCAN_W 8
 #endif
-#ifndef SCAN_V1
-#define SCAN_V1 1
-#endif
 #ifndef SCAN_SF
 #define SCAN_SF 16
 #endif
@@ -59,12 +56,20 @@ constexpr int kShortThreads = 128;
 #ifndef SCAN_BB
 #define SCAN_BB 1
 #endif
+#ifndef SCAN_U
+#define SCAN_U 8
+#endif
+#ifndef SCAN_UB
+#define SCAN_UB 4
+#endif
+#ifndef SCAN_BU
+#define SCAN_BU 1
+#endif
 constexpr int kWarps = SCAN_W;
-// Columns of a thread: 8 bytes of a row, or one where the rows do not allow that.  Its steps: what its registers hold twice (coefficients of
-// this tile, raw values of the next).
-template <class T> constexpr int kWide = 8 / sizeof(T);
-template <int VC, bool BACK> constexpr int kStepsOf = (BACK ? SCAN_SB : SCAN_SF) * (VC == 1 ? SCAN_V1 : 1);
-template <bool BACK> constexpr int kBlocksOf = BACK ? SCAN_BB : SCAN_BF;
+template <class T> constexpr int kWide = 8 / sizeof(T);      // columns of a thread: 8 bytes of a row
+// Steps of a thread, and blocks on an SM that registers are kept free for.  ALIGNED rows are staged in shared memory, others in registers.
+template <bool ALIGNED, bool BACK> constexpr int kStepsOf = ALIGNED ? (BACK ? SCAN_SB : SCAN_SF) : BACK ? SCAN_UB : SCAN_U;
+template <bool ALIGNED, bool BACK> constexpr int kBlocksOf = ALIGNED ? (BACK ? SCAN_BB : SCAN_BF) : SCAN_BU;
 #ifndef SCAN_D
 #define SCAN_D 1
 #endif
@@ -222,15 +227,17 @@ template <bool GIVEN, int VC> __device__ __forceinline__ void slopes(const Coef<
   wc = k.q * (fma_(k.n, V::all(-1.0f), V::all(1.0f)) * (k.n + V::all(1.0f)));
 }
 
-template <int VC> __device__ __forceinline__ F<VC> load_state(const float* p, unsigned col) {
+// n of VC states (the others are zero, or not stored)
+template <int VC> __device__ __forceinline__ F<VC> load_state(const float* p, unsigned col, int n = VC) {
   F<VC> f;
 #pragma unroll
-  for (int v = 0; v < VC; ++v) f.at(v) = p ? p[col + v] : 0.f;
+  for (int v = 0; v < VC; ++v) f.at(v) = p && v < n ? p[col + v] : 0.f;
   return f;
 }
-template <int VC> __device__ __forceinline__ void store_state(float* p, unsigned col, F<VC> f) {
+template <int VC> __device__ __forceinline__ void store_state(float* p, unsigned col, const F<VC>& f, int n = VC) {
 #pragma unroll
-  for (int v = 0; v < VC; ++v) p[col + v] = f.at(v);
+  for (int v = 0; v < VC; ++v)
+    if (v < n) p[col + v] = f.at(v);
 }
 
 // What a thread knows of its columns: the first one, its sequence and unit, the steps of that sequence
@@ -319,8 +326,7 @@ __device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, uns
 // The state in front of tile k of column tile c, for the warp's columns: carried from the last published state through the pairs after
 // it.  Words of a tile are published together, so one of them (the first column's) tells the lanes how far back to go.  A tile that found
 // the state in front of it at once publishes no pair, only its state: whoever misses a word looks again from the start.
-template <int VC> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, int c, int lane) {
-  const i64 row = (i64)a.nc * (32 * VC), col = (i64)c * (32 * VC);
+template <int VC> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, i64 row, i64 col, int lane) {
   uint64_t t0 = 0;
   for (unsigned round = 0; !waited_too_long(a, lane, round, t0); ++round) {
     int from = -1;                             // the tile whose state is taken
@@ -371,15 +377,14 @@ __device__ __forceinline__ Place place_of(const ScanArgs& a, unsigned tile, int 
   p.k = (int)(tile / (unsigned)a.nc);
   p.c = (int)(tile - (unsigned)p.k * (unsigned)a.nc);
   const unsigned col = (unsigned)p.c * (unsigned)columns;
-  p.b = col / (unsigned)a.H;
-  p.u = col - p.b * (unsigned)a.H;
+  p.b = col / (unsigned)a.Hp;
+  p.u = col - p.b * (unsigned)a.Hp;
   return p;
 }
 
-template <class T, bool GIVEN, int VC, bool BACK>
-__global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
-  constexpr bool STAGED = VC * sizeof(T) == 8;
-  constexpr int S = kStepsOf<VC, BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
+template <class T, bool GIVEN, bool STAGED, bool BACK>
+__global__ void __launch_bounds__(kWarps * 32, kBlocksOf<STAGED, BACK>) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
+  constexpr int VC = kWide<T>, S = kStepsOf<STAGED, BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
   extern __shared__ __align__(16) char stage[];      // [tiles ahead][ARRAYS][S][threads] words of 8 bytes
   constexpr unsigned ALL = (1u << S) - 1u;
   using V = F<VC>;
@@ -393,77 +398,107 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
   const auto time_of = [&](int i) { return BACK ? a.T - 1 - i : i; };
 
   // where the thread stands in a tile: sequence and unit of its columns, its first step counted from the scan's start
-  struct Spot { unsigned b, u; int i0; bool live; };
-  const auto spot_of = [&](const Place& p) {
+  struct Spot { unsigned b, u; int i0, n; };      // n: columns of the thread that exist
+  const auto spot_of = [&](const Place& p, int column) {
     Spot s;
     s.b = p.b;
-    s.u = p.u + lane * VC;
-    if (s.u >= (unsigned)a.H) {                // the tile reaches into the next sequences
-      const unsigned n = s.u / (unsigned)a.H;
+    s.u = p.u + column;
+    if (s.u >= (unsigned)a.Hp) {               // the tile reaches into the next sequences
+      const unsigned n = s.u / (unsigned)a.Hp;
       s.b += n;
-      s.u -= n * (unsigned)a.H;
+      s.u -= n * (unsigned)a.Hp;
     }
     s.i0 = p.k * TT + warp * S;
-    s.live = s.b < (unsigned)a.B;
+    s.n = s.b >= (unsigned)a.B ? 0 : STAGED ? VC : min(VC, a.H - (int)s.u);
     return s;
   };
   const auto at = [&](const ScanRows& r, const Spot& s, int t) { return reinterpret_cast<T*>(r.p) + ((i64)t * r.ts + (i64)s.b * r.bs + s.u); };
 
-  // The thread's own steps of a tile, as they come from memory.  Rows that allow it are staged in shared memory by asynchronous copies
-  // (a thread reads back what it copied itself, so nobody waits for anybody), which leaves the registers to the tile in work.
-  const unsigned slot0 = (unsigned)__cvta_generic_to_shared(stage) + threadIdx.x * 8u;
-  constexpr unsigned kSlot = kWarps * 32 * 8u, kTile = ARRAYS * S * kSlot;
+  // The warp's steps of a tile, as they come from memory.  Rows that allow it are staged in shared memory by asynchronous copies of 16
+  // bytes (two rows of a warp at a time, past L1), which leaves the registers to the tile in work; only the warp itself waits for them.
+  constexpr unsigned kRow = CT * sizeof(T), kPieces = kRow / 16, kRows = STAGED ? 32 / kPieces : 1;      // bytes of a row, copies of a row, rows at a time
+  constexpr unsigned kArray = S * kRow, kTile = kWarps * ARRAYS * kArray;
+  static_assert(!STAGED || (kRow % 16 == 0 && 32 % kPieces == 0 && S % kRows == 0), "whole copies of whole rows");
+  char* const slice = stage + warp * (ARRAYS * kArray);
+  const unsigned slot0 = (unsigned)__cvta_generic_to_shared(slice) + (lane / kPieces) * kRow + (lane % kPieces) * 16u;
   Vec<T, VC> regs[STAGED ? 1 : ARRAYS][STAGED ? 1 : S];
-  const auto bring = [&](unsigned d, int array, int s, const T* p, bool in) {
-    if (STAGED) {
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(slot0 + d * kTile + (array * S + s) * kSlot), "l"(p), "r"(in ? 8 : 0) : "memory");
-    } else {
-      regs[STAGED ? 0 : array][STAGED ? 0 : s] = in ? load<T, VC>(p) : zeros<T, VC>();
-    }
-  };
   const auto raw = [&](unsigned d, int array, int s) {
     if (!STAGED) return regs[STAGED ? 0 : array][STAGED ? 0 : s];
-    return *reinterpret_cast<const Vec<T, VC>*>(stage + d * kTile + threadIdx.x * 8u + (array * S + s) * kSlot);
+    return *reinterpret_cast<const Vec<T, VC>*>(slice + d * kTile + array * kArray + s * kRow + lane * sizeof(Vec<T, VC>));
   };
-  // -> which of the steps lie in the sequence, and (from bit 16 on) which of them start one
-  const auto fetch = [&](const Spot& s, unsigned d) {
-    unsigned inside, fresh;
-    const int len = !s.live ? 0 : a.lengths ? min(max(a.lengths[s.b], 0), a.T) : a.T;
-    // steps i0 .. i0 + S - 1 of the scan that lie in the sequence
+  // steps i0 .. i0 + S - 1 of the scan that lie in the sequence
+  const auto inside_of = [&](const Spot& s) {
+    const int len = s.n == 0 ? 0 : a.lengths ? min(max(a.lengths[s.b], 0), a.T) : a.T;
     const int lo = BACK ? max(0, a.T - len - s.i0) : 0, hi = BACK ? min(S, a.T - s.i0) : min(S, len - s.i0);
-    inside = hi > lo ? (ALL >> (S - hi)) & (ALL << lo) : 0u;
-    fresh = 0u;
+    return hi > lo ? (ALL >> (S - hi)) & (ALL << lo) : 0u;
+  };
+  // -> which of the thread's steps lie in the sequence, and (from bit 16 on) which of them start one
+  const auto fetch = [&](const Place& p, unsigned d) {
+    const Spot s = spot_of(p, lane * VC);
+    const unsigned inside = inside_of(s);
+    unsigned fresh = 0u;
     const int t0 = time_of(s.i0);
-    const T *pg = at(a.gate, s, t0), *pc = at(a.cand, s, t0);
-    const T *ph = BACK ? at(a.h, s, t0 - 1) : nullptr, *ps = BACK ? at(a.seed, s, t0) : nullptr;
-    const i64 dg = BACK ? -a.gate.ts : a.gate.ts, dc = BACK ? -a.cand.ts : a.cand.ts;
-    const bool seeded = BACK && a.seed.p;
-    if (__all_sync(0xffffffffu, inside == ALL && !cut && (!BACK || (t0 >= S && seeded)))) {
+    if (cut) {                                 // all of them asked for before the first is looked at
+      uint8_t mark[S];
 #pragma unroll
       for (int i = 0; i < S; ++i) {
-        bring(d, 0, i, pg + i * dg, true);
-        bring(d, 1, i, pc + i * dc, true);
-        if (BACK) {
-          bring(d, 2, i, ph - i * a.h.ts, true);
-          bring(d, 3, i, ps - i * a.seed.ts, true);
-        }
+        const uint8_t* p = reinterpret_cast<const uint8_t*>(a.reset.p);
+        mark[i] = p[(inside >> i & 1u) ? (i64)time_of(s.i0 + i) * a.reset.ts + (i64)s.b * a.reset.bs : 0];
       }
+#pragma unroll
+      for (int i = 0; i < S; ++i) fresh |= mark[i] && (inside >> i & 1u) ? 1u << i : 0u;
+    }
+    if constexpr (STAGED) {
+      const Spot mine = spot_of(p, (lane % kPieces) * (16 / (int)sizeof(T)));
+      const int r = (int)(lane / kPieces), t1 = BACK ? t0 - r : t0 + r;
+      const auto bring = [&](int array, const ScanRows& from, int t, bool there, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        const unsigned valid = WHOLE ? ALL : inside_of(mine);
+        const T* q = at(from, mine, t);
+        const i64 dq = (BACK ? -from.ts : from.ts) * (i64)kRows;
+        const unsigned to = slot0 + d * kTile + array * kArray;
+#pragma unroll
+        for (int i = 0; i < S / (int)kRows; ++i) {
+          if (WHOLE) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + i * (kRows * kRow)), "l"(q + i * dq) : "memory");
+          } else {                             // what lies outside is not read: zeros stand in for it
+            const int step = i * (int)kRows + r;
+            const bool in = there && (valid >> step & 1u) && (array != 2 || time_of(mine.i0 + step) > 0);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + i * (kRows * kRow)), "l"(in ? q + i * dq : reinterpret_cast<const T*>(a.gate.p)), "r"(in ? 16 : 0) : "memory");
+          }
+        }
+      };
+      if (__all_sync(0xffffffffu, inside == ALL && (!BACK || (t0 >= S && a.seed.p)))) {
+        bring(0, a.gate, t1, true, std::true_type{});
+        bring(1, a.cand, t1, true, std::true_type{});
+        if (BACK) { bring(2, a.h, t1 - 1, true, std::true_type{}); bring(3, a.seed, t1, true, std::true_type{}); }
+      } else {
+        bring(0, a.gate, t1, true, std::false_type{});
+        bring(1, a.cand, t1, true, std::false_type{});
+        if (BACK) { bring(2, a.h, t1 - 1, true, std::false_type{}); bring(3, a.seed, t1, a.seed.p != nullptr, std::false_type{}); }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     } else {
-      // (what is not inside is not read: the address of the array's first element stands in for it)
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         const bool in = inside >> i & 1u;
-        bring(d, 0, i, in ? pg + i * dg : reinterpret_cast<const T*>(a.gate.p), in);
-        bring(d, 1, i, in ? pc + i * dc : reinterpret_cast<const T*>(a.cand.p), in);
-        if (BACK) {
-          const bool before = in && t0 - i > 0, sd = in && seeded;
-          bring(d, 2, i, before ? ph - i * a.h.ts : reinterpret_cast<const T*>(a.h.p), before);
-          bring(d, 3, i, sd ? ps - i * a.seed.ts : reinterpret_cast<const T*>(a.gate.p), sd);
+        const int t = time_of(s.i0 + i);
+        const auto take = [&](int array, const ScanRows& from, int t, bool there) {
+          Vec<T, VC> x = zeros<T, VC>();
+          const T* q = at(from, s, t);
+#pragma unroll
+          for (int v = 0; v < VC; ++v)
+            if (there && v < s.n) x.x[v] = q[v];
+          regs[array][i] = x;
+        };
+        take(0, a.gate, t, in);
+        take(1, a.cand, t, in);
+        if constexpr (BACK) {
+          take(2, a.h, t - 1, in && t > 0);
+          take(3, a.seed, t, in && a.seed.p);
         }
-        if (cut && in && reinterpret_cast<const uint8_t*>(a.reset.p)[(i64)time_of(s.i0 + i) * a.reset.ts + (i64)s.b * a.reset.bs]) fresh |= 1u << i;
       }
     }
-    if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory");
     return inside | fresh << 16;
   };
 
@@ -485,7 +520,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
 #pragma unroll
     for (int i = 0; i < D; ++i) {
       const Place p = place[i];
-      ahead[i] = p.k >= 0 ? fetch(spot_of(p), i) : none();
+      ahead[i] = p.k >= 0 ? fetch(p, i) : none();
     }
   }
 
@@ -506,39 +541,51 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
 
     V ca[S], cb[S], wg[SB], wc[SB];            // cb: b, backward: the seed
     if (STAGED) asm volatile("cp.async.wait_group %0;" :: "n"(D - 1) : "memory");      // (all but the D - 1 last groups)
+    __syncwarp();
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const Coef<VC> o = coefficients<GIVEN, T, VC>(raw(d, 0, s), raw(d, 1, s), a);
       ca[s] = o.a;
       if (BACK) {
         V hp = raw(d, 2, s).get();
-        if (ODD && time_of(now.i0 + s) == 0 && (in_now >> s & 1u)) hp = load_state<VC>(a.h0, now.b * (unsigned)a.H + now.u);
-        if (ODD && (fresh_now >> s & 1u)) hp = V::all(0.f);
+        if (ODD && time_of(now.i0 + s) == 0 && (in_now >> s & 1u)) hp = load_state<VC>(a.h0, now.b * (unsigned)a.H + now.u, now.n);
+        if (ODD && cut) hp = each(hp, [&](float x, int) { return (fresh_now >> s & 1u) ? 0.f : x; });
         cb[s] = raw(d, 3, s).get();
         slopes<GIVEN, VC>(o, hp, wg[BACK ? s : 0], wc[BACK ? s : 0]);
       } else {
         cb[s] = o.b;
       }
       if (ODD) {
-        if (!(in_now >> s & 1u)) { ca[s] = V::all(1.f); cb[s] = V::all(0.f); }
-        if (fresh_now >> s & 1u) ca[s] = V::all(0.f);
+        const bool in = in_now >> s & 1u, fr = fresh_now >> s & 1u;
+        ca[s] = each(ca[s], [&](float x, int) { return !in ? 1.f : fr ? 0.f : x; });
+        cb[s] = each(cb[s], [&](float x, int) { return in ? x : 0.f; });
       }
     }
+    if (STAGED) __syncwarp();                  // the slot has been read
     unsigned theirs = 0u;
     if (a.deep) {
       const Place later = place[(turn + D) % RING];
-      theirs = later.k >= 0 ? fetch(spot_of(later), d) : none();
+      theirs = later.k >= 0 ? fetch(later, d) : none();
     }
 
     // one step of the scan: forward h -> a h + b, backward mu -> a (mu + seed)
     const auto step = [&](int s, V h) {
-      if (ODD && (fresh_now >> s & 1u)) return BACK ? V::all(0.f) : cb[s];
+      if (ODD && cut) {                        // (a = 0 would not stop a NaN or an infinity)
+        const bool fr = fresh_now >> s & 1u;
+#pragma unroll
+        for (int v = 0; v < VC; ++v) h.at(v) = fr ? 0.f : h.at(v);
+        if (BACK) {
+          const V m = ca[s] * (h + cb[s]);
+          return each(m, [&](float x, int) { return fr ? 0.f : x; });
+        }
+      }
       return BACK ? ca[s] * (h + cb[s]) : fma_(ca[s], h, cb[s]);
     };
     V A = V::all(1.f), h = V::all(0.f);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      A = ODD && (fresh_now >> s & 1u) ? V::all(0.f) : s == 0 ? ca[s] : ca[s] * A;
+      A = s == 0 ? ca[s] : ca[s] * A;
+      if (ODD && cut) A = each(A, [&](float x, int) { return (fresh_now >> s & 1u) ? 0.f : x; });
       h = step(s, h);
     }
 #pragma unroll
@@ -560,7 +607,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
     }
     if (k == 0) {
       const float* first = BACK ? a.dhT : a.h0;
-      h = now.live ? load_state<VC>(first, now.b * (unsigned)a.H + now.u) : V::all(0.f);
+      h = load_state<VC>(first, now.b * (unsigned)a.H + now.u, now.n);
     } else {
       bool known = true;
 #pragma unroll
@@ -573,7 +620,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
 #pragma unroll
           for (int v = 0; v < VC; ++v) st_pair(a.pairs + word + v, whole[v]);
         }
-        h = look_back<VC>(a, k, c, lane);
+        h = look_back<VC>(a, k, row, (i64)c * CT, lane);
       }
     }
     if (speaker) {
@@ -582,13 +629,23 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
     }
 #pragma unroll
     for (int w = 0; w < kWarps - 1; ++w) {
-      if (w < warp) {
 #pragma unroll
-        for (int v = 0; v < VC; ++v) h.at(v) = through(pair[buf][w][lane * VC + v], h.at(v), cut);
+      for (int v = 0; v < VC; ++v) {
+        const float2 p = pair[buf][w][lane * VC + v];
+        if (w < warp) h.at(v) = through(p, h.at(v), cut);
       }
     }
     T *po = at(BACK ? a.dgate : a.h, now, time_of(now.i0)), *pw = BACK ? at(a.dcand, now, time_of(now.i0)) : nullptr;
     const i64 dout = BACK ? -a.dgate.ts : a.h.ts;
+    const auto put = [&](T* p, const V& x) {
+      if constexpr (STAGED) {
+        store<T, VC>(p, x);
+      } else {
+#pragma unroll
+        for (int v = 0; v < VC; ++v)
+          if (v < now.n) p[v] = from_f32<T>(x.at(v));
+      }
+    };
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       V x, y;
@@ -602,16 +659,18 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
       bool write = true;
       if (ODD) {
         const int t = time_of(now.i0 + s);
-        write = now.live && t >= 0 && t < a.T;
-        if (!(in_now >> s & 1u)) x = y = V::all(0.f);
+        write = now.n > 0 && t >= 0 && t < a.T;
+        const bool in = in_now >> s & 1u;
+        x = each(x, [&](float v, int) { return in ? v : 0.f; });
+        if (BACK) y = each(y, [&](float v, int) { return in ? v : 0.f; });
       }
       if (write) {
-        store<T, VC>(po + s * dout, x);
-        if (BACK) store<T, VC>(pw - s * a.dcand.ts, y);
+        put(po + s * dout, x);
+        if (BACK) put(pw - s * a.dcand.ts, y);
       }
     }
     float* last = BACK ? a.dh0 : a.hT;
-    if (last && k + 1 == a.nk && warp == kWarps - 1 && now.live) store_state<VC>(last, now.b * (unsigned)a.H + now.u, h);
+    if (last && k + 1 == a.nk && warp == kWarps - 1) store_state<VC>(last, now.b * (unsigned)a.H + now.u, h, now.n);
     return theirs;
   };
   for (unsigned turn = 0, d = 0;; ++turn, d = d + 1 == D ? 0 : d + 1) {
@@ -621,9 +680,9 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<BACK>) scan_tile_kernel
     }
     const Place here = place[turn % RING];
     if (here.k < 0) break;
-    const Spot now = spot_of(here);
+    const Spot now = spot_of(here, lane * VC);
     if (!a.deep) {
-      ahead[0] = fetch(now, d);
+      ahead[0] = fetch(here, d);
 #pragma unroll
       for (int i = 1; i < D; ++i) none();
     }
@@ -692,9 +751,11 @@ int copy_state(float* dst, const float* src, size_t n, cudaStream_t s) {
   return e == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
+constexpr int kWidest = 32 * 4;
 // Workspace: counter | states | pairs, filled with kNone.  Columns are padded to the wider column tile, time to the shortest one.
-constexpr int kLeastSteps = kStepsOf<2, true> * kWarps;
-static_assert(kLeastSteps <= kStepsOf<2, false> * kWarps && kLeastSteps <= kStepsOf<1, true> * kWarps, "the shortest tile sizes the workspace");
+constexpr int kLeastSteps = kStepsOf<false, true> * kWarps;
+static_assert(kLeastSteps <= kStepsOf<true, true> * kWarps && kLeastSteps <= kStepsOf<true, false> * kWarps && kLeastSteps <= kStepsOf<false, false> * kWarps,
+              "the shortest tile sizes the workspace");
 struct ScanSpace { size_t states, pairs, total; };
 ScanSpace scan_space(i64 nk, i64 padded) {
   ScanSpace s;
@@ -715,10 +776,10 @@ int* scan_status_ptr() {
   return g_scan_status_ptrs[dev];
 }
 
-// several columns a thread where rows allow it: units and strides whole words of 8 bytes, all addresses on such words
+// several columns a thread and asynchronous copies where rows allow it: units and strides whole words of 16 bytes, all addresses on such words
 bool wide_columns(const ScanArgs& a, int dtype) {
-  const int n = 8 / (int)elem_size(dtype);
-  const auto fits = [&](const ScanRows& r) { return !r.p || (((uintptr_t)r.p & 7u) == 0 && r.ts % n == 0 && r.bs % n == 0); };
+  const int n = 16 / (int)elem_size(dtype);
+  const auto fits = [&](const ScanRows& r) { return !r.p || (((uintptr_t)r.p & 15u) == 0 && r.ts % n == 0 && r.bs % n == 0); };
   return a.H % n == 0 && fits(a.gate) && fits(a.cand) && fits(a.h) && fits(a.seed) && fits(a.dgate) && fits(a.dcand);
 }
 
@@ -737,17 +798,22 @@ template <class K> int resident_blocks(K kern, int threads, int smem, int (&know
   return known[dev];
 }
 
-template <class T, bool GIVEN, int VC, bool BACK> int launch_scan(ScanArgs& a, void* ws, size_t ws_bytes, cudaStream_t s) {
-  const i64 cols = (i64)a.B * a.H;
+template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs& a, void* ws, size_t ws_bytes, cudaStream_t s) {
+  constexpr int VC = kWide<T>;
   if (a.T <= kShort) {
-    scan_short_kernel<T, GIVEN, VC, BACK><<<(unsigned)((cols / VC + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
+    constexpr int VS = ALIGNED ? VC : 1;
+    const i64 cols = (i64)a.B * a.H;
+    scan_short_kernel<T, GIVEN, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
   } else {
-    constexpr int steps = kStepsOf<VC, BACK> * kWarps;
-    const i64 nc = (cols + 32 * VC - 1) / (32 * VC), nk = ((i64)a.T + steps - 1) / steps;
+    constexpr int steps = kStepsOf<ALIGNED, BACK> * kWarps, wide = 32 * VC;
+    a.Hp = (a.H + VC - 1) / VC * VC;
+    const i64 cols = (i64)a.B * a.Hp;
+    if (cols >= ((i64)1 << 31)) return MGRIT_UNSUPPORTED;
+    const i64 nc = (cols + wide - 1) / wide, nk = ((i64)a.T + steps - 1) / steps;
     if (nk * nc >= INT32_MAX) return MGRIT_UNSUPPORTED;
     a.nk = (int)nk; a.nc = (int)nc;
     if (nk > 1) {
-      const ScanSpace sp = scan_space(nk, nc * 32 * VC);
+      const ScanSpace sp = scan_space(nk, nc * wide);
       if (!ws || ((uintptr_t)ws & 255u)) return MGRIT_INVALID_ARG;
       if (ws_bytes < sp.total) return MGRIT_WORKSPACE_TOO_SMALL;
       char* w = static_cast<char*>(ws);
@@ -758,12 +824,12 @@ template <class T, bool GIVEN, int VC, bool BACK> int launch_scan(ScanArgs& a, v
       if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
     }
     static int known[kMaxDevices];
-    constexpr int smem = VC * sizeof(T) == 8 ? kAhead * (BACK ? 4 : 2) * kStepsOf<VC, BACK> * kWarps * 32 * 8 : 0;
-    const int most = resident_blocks(scan_tile_kernel<T, GIVEN, VC, BACK>, kWarps * 32, smem, known);
+    constexpr int smem = ALIGNED ? kAhead * (BACK ? 4 : 2) * kStepsOf<ALIGNED, BACK> * kWarps * 32 * 8 : 0;
+    const int most = resident_blocks(scan_tile_kernel<T, GIVEN, ALIGNED, BACK>, kWarps * 32, smem, known);
     if (most <= 0) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
     // every block gets four tiles or more: enough that the first ones to run may take several at once
     a.deep = nk * nc >= 4 * (i64)most;
-    scan_tile_kernel<T, GIVEN, VC, BACK><<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
+    scan_tile_kernel<T, GIVEN, ALIGNED, BACK><<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
   }
   count_launch();
   return cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
@@ -779,9 +845,8 @@ int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cud
     using T = decltype(tag);
     const auto pick = [&](auto g) {
       constexpr bool G = decltype(g)::value;
-      constexpr int W = kWide<T>;
-      rc = wide ? (back ? launch_scan<T, G, W, true>(a, ws, ws_bytes, s) : launch_scan<T, G, W, false>(a, ws, ws_bytes, s))
-               : (back ? launch_scan<T, G, 1, true>(a, ws, ws_bytes, s) : launch_scan<T, G, 1, false>(a, ws, ws_bytes, s));
+      rc = wide ? (back ? launch_scan<T, G, true, true>(a, ws, ws_bytes, s) : launch_scan<T, G, true, false>(a, ws, ws_bytes, s))
+               : (back ? launch_scan<T, G, false, true>(a, ws, ws_bytes, s) : launch_scan<T, G, false, false>(a, ws, ws_bytes, s));
     };
     if (given) pick(std::true_type{}); else pick(std::false_type{});
   });
@@ -810,7 +875,7 @@ extern "C" {
 
 size_t gated_scan_workspace_bytes(int32_t T, int32_t B, int32_t H) {
   if (!mg::scan_sizes_served(T, B, H) || T <= mg::kLeastSteps || B == 0) return 0;
-  return mg::scan_space(((mg::i64)T + mg::kLeastSteps - 1) / mg::kLeastSteps, ((mg::i64)B * H + 127) / 128 * 128).total;
+  return mg::scan_space(((mg::i64)T + mg::kLeastSteps - 1) / mg::kLeastSteps, ((mg::i64)B * ((H + 3) / 4 * 4) + mg::kWidest - 1) / mg::kWidest * mg::kWidest).total;
 }
 
 int gated_scan_forward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream) {
