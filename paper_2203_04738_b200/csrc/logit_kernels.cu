@@ -1,13 +1,388 @@
 // Operators over rows of logits: log probabilities of given tokens with entropy and top alternatives, their gradient, and
 // distillation from a teacher's top logits.
+//
+// All are bound by HBM (a row is read once, gradients are written once) with one or two exponentials an element, which take up to three
+// quarters of that time (16 a cycle and SM).  Rows of up to 16 x kThreads x kVecs vectors are held in registers:
+//  * short rows (V <= 1024): a group of 8 or 32 lanes has a row;
+//  * longer ones: a block, or a cluster of up to 16 blocks that share a row and meet through distributed shared memory.  A thread
+//    loads all of its 16-byte vectors at once, so that the largest logit, the sums, the top alternatives and the gradient are all
+//    formed without reading a row again, and without the rescaling that running sums need.  Few rows are split over more blocks than
+//    they need, so that a single token's row of 131072 is read by 16 SMs;
+//  * rows beyond that: a block per row in several passes (only their first one from HBM, the others mostly from L2).
+// Rows may start anywhere: vectors are aligned in memory, the first and the last one of a row are read element by element.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "elem.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace mg {
 namespace {
 
 constexpr int kMaxTop = 128, kMaxTeacher = 1024;
+constexpr int kVecs = 8;                       // 16-byte vectors of a thread
+constexpr int kMaxCluster = 16;
+constexpr int kShortRow = 1024;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
+// Order of the alternatives as one whole number: the value's bits so that they rise with the value (-0 as +0, NaN below -inf), then the
+// token, lower ones first.  Every key of a row is different and above zero.
+__device__ __forceinline__ unsigned value_key(float x) {
+  x += 0.f;
+  const int b = __float_as_int(x);
+  return x != x ? 0u : (unsigned)(b < 0 ? b ^ 0x7fffffff : b) ^ 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long top_key(float x, int v) { return ((unsigned long long)value_key(x) << 32) | (unsigned)(0xffffffffu - (unsigned)v); }
+__device__ __forceinline__ int key_token(unsigned long long k) { return (int)(0xffffffffu - (unsigned)k); }
+
+// ---- vectors of 16 bytes ---------------------------------------------------------------------------------------------------------
+
+template <class T> struct V16 {
+  static constexpr int E = 16 / sizeof(T);     // elements
+  uint4 w;
+  __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
+  __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
+  __device__ __forceinline__ T& raw(int i) { return reinterpret_cast<T*>(&w)[i]; }
+};
+// the largest element, NaN where there is one (two 16-bit values an instruction)
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b, __nv_bfloat16) { unsigned y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b)); return y; }
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b, __half) { unsigned y; asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b)); return y; }
+template <class T> __device__ __forceinline__ float max_of(const V16<T>& v) {
+  if constexpr (sizeof(T) == 4) {
+    return max_nan(max_nan(v.get(0), v.get(1)), max_nan(v.get(2), v.get(3)));
+  } else {
+    V16<T> m;
+    m.w.x = max2(max2(v.w.x, v.w.y, T{}), max2(v.w.z, v.w.w, T{}), T{});
+    return max_nan(m.get(0), m.get(1));
+  }
+}
+
+// A row's place in memory: `skip` elements lie between the 16-byte word in which it starts and its first element
+template <class T> struct RowAt {
+  T* base;                                     // that word
+  int skip, vecs;                              // vectors that hold some of the row
+  __device__ __forceinline__ RowAt(T* row, int V) {
+    skip = (int)(((uintptr_t)row & 15u) / sizeof(T));
+    base = row - skip;
+    vecs = (int)(((i64)V + skip + V16<T>::E - 1) / V16<T>::E);
+  }
+};
+template <class T> __device__ __forceinline__ V16<T> load_vec(const T* row, const RowAt<const T>& at, int i, int V) {
+  constexpr int E = V16<T>::E;
+  V16<T> v;
+  if (i > 0 && i + 1 < at.vecs) {
+    v.w = __ldcs(reinterpret_cast<const uint4*>(at.base) + i);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int k = i * E + e - at.skip;
+      v.raw(e) = k >= 0 && k < V ? row[k] : from_f32<T>(-INFINITY);
+    }
+  }
+  return v;
+}
+
+// ---- reductions over a block -----------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// Statistics of some of a row's logits: the largest, m; s = sum 2^((x - m) log2 e); w = sum of the same terms times their exponents.
+// A part without any logit above -inf has m = -inf and s = 0.
+struct Stats { float m, s, w; };
+__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ Stats joined(const Stats& a, const Stats& b) {
+  const float m = max_nan(a.m, b.m), r = ref_of(m);
+  const float da = (a.m - r) * kLog2e, db = (b.m - r) * kLog2e, fa = ex2(da), fb = ex2(db);
+  Stats o;
+  o.m = m;
+  o.s = a.s * fa + b.s * fb;
+  o.w = (fa == 0.f ? 0.f : fa * fmaf(a.s, da, a.w)) + (fb == 0.f ? 0.f : fb * fmaf(b.s, db, b.w));      // (da may be -inf)
+  return o;
+}
+// log s of a row, NaN where the row holds a NaN or +inf
+__device__ __forceinline__ float log_sum(const Stats& t) { return t.m != t.m || t.m == INFINITY ? __int_as_float(0x7fc00000) : logf(t.s); }
+
+struct LogprobArgs {
+  int N, V, top; i64 ld;
+  const int32_t* tokens; float *logprob, *entropy, *lse, *top_logprob; int32_t* top_id;
+};
+// log probability of a logit of the row (x - max, then - log of the sum: x - lse would lose the second part where the row lies far from zero)
+__device__ __forceinline__ float logprob_of(float x, const Stats& t, float ls) { return t.m == -INFINITY ? -INFINITY : (x - t.m) - ls; }
+template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& a, const T* x, int r, const Stats& t) {
+  const float ls = log_sum(t);
+  if (a.lse) a.lse[r] = t.m == -INFINITY ? -INFINITY : t.m + ls;
+  if (a.entropy) a.entropy[r] = t.m == -INFINITY ? 0.f : ls - kLn2 * (t.w / t.s);
+  if (a.tokens) {
+    const int v = a.tokens[r];
+    a.logprob[r] = v >= 0 && v < a.V ? logprob_of(to_f32(x[v]), t, ls) : 0.f;
+  }
+}
+
+// ---- log probabilities: rows in the registers of a block or a cluster --------------------------------------------------------------
+
+constexpr int kList = 2048;                    // candidates that a block holds: its own, or those of a cluster
+static_assert(kList >= kMaxCluster * kMaxTop, "the lists of a whole cluster");
+
+// Writes the `top` largest of n keys, in order, to out(rank, key): each key counts those above it.
+template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsigned long long* list, int n, int top, Out&& out) {
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const unsigned long long k = list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > k;
+    if (rank < top) out(rank, k);
+  }
+}
+
+// The top alternatives: a warp's lanes have the largest logit each of their own share, and the warp's j-th largest of these, j = top /
+// warps rounded up, is a bound: at least j of its logits reach it.  So at least `top` logits reach the lowest of the warps' bounds, and
+// those that do are few (some hundred of 32768 random ones for top = 20); they are put in order by counting.  Where ties or a NaN
+// make them many, the largest is taken out `top` times instead.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
+  constexpr int E = V16<T>::E, NW = NT / 32;
+  __shared__ unsigned long long list[kList];
+  __shared__ unsigned long long best[kMaxTop];
+  __shared__ float wmax[NW], wbound[NW], wsum[NW], wdot[NW];
+  __shared__ Stats part;
+  __shared__ int count;
+  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait();
+  pdl_trigger();
+  const T* row = logits + (i64)r * a.ld;
+  const RowAt<const T> at(row, a.V);
+  const int share = (at.vecs + cluster - 1) / cluster, lo = rank * share, n = max(0, min(at.vecs - lo, share));      // the block's vectors
+  V16<T> x[kVecs];
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q) {
+    const int i = q * NT + threadIdx.x;
+    if (i < n) x[q] = load_vec<T>(row, at, lo + i, a.V);
+  }
+  if (threadIdx.x == 0) count = 0;
+  float m = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q)
+    if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
+  const float mine = m;
+  m = warp_max(m);
+  if (lane == 0) wmax[warp] = m;
+  if (a.top > 0) {
+    // the warp's j-th largest of its lanes' largest logits; warps without logits have no say
+    const int warps = min(NW, (n + 31) / 32), j = (a.top + max(warps, 1) - 1) / max(warps, 1);
+    unsigned k = value_key(mine), b = 0u;
+    for (int i = 0; i < min(j, 32); ++i) {
+      b = __reduce_max_sync(0xffffffffu, k);
+      const unsigned who = __ballot_sync(0xffffffffu, k == b);
+      if (lane == __ffs(who) - 1) k = 0u;
+    }
+    if (j > 32) b = 0u;
+    const unsigned u = b ^ 0x80000000u;
+    if (lane == 0) wbound[warp] = warp * 32 < n ? (b == 0u ? -INFINITY : __uint_as_float((int)u < 0 ? u ^ 0x7fffffffu : u)) : INFINITY;
+  }
+  __syncthreads();
+  m = wmax[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) m = max_nan(m, wmax[w]);
+  // sums: exponents stop at -150, where the terms are zero (a term of -inf would make 0 x inf of its product)
+  const float m0 = ref_of(m);
+  float s = 0.f, w = 0.f;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q) {
+    if (q * NT + threadIdx.x < n) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float t = fmaxf((x[q].get(e) - m0) * kLog2e, -150.f), y = ex2(t);
+        s += y;
+        w = fmaf(y, t, w);
+      }
+    }
+  }
+  s = warp_sum(s);
+  w = warp_sum(w);
+  if (lane == 0) { wsum[warp] = s; wdot[warp] = w; }
+  float bound = INFINITY;
+  if (a.top > 0) {
+#pragma unroll
+    for (int q = 0; q < NW; ++q) bound = fminf(bound, wbound[q]);
+    if (mine >= bound) {
+#pragma unroll
+      for (int q = 0; q < kVecs; ++q) {
+        if (q * NT + threadIdx.x < n && max_of(x[q]) >= bound) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
+            if (x[q].get(e) >= bound && v >= 0 && v < a.V) {
+              const int at_ = atomicAdd(&count, 1);
+              if (at_ < kList) list[at_] = top_key(x[q].get(e), v);
+            }
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    Stats t{m, 0.f, 0.f};
+    for (int q = 0; q < NW; ++q) { t.s += wsum[q]; t.w += wdot[q]; }
+    if (m == -INFINITY) t.s = t.w = 0.f;
+    part = t;
+  }
+  const int first = max(0, lo * E - at.skip), end = min(a.V, (lo + n) * E - at.skip), have = min(a.top, max(0, end - first));      // the block's own best
+  if (a.top > 0) {
+    const int found = count;
+    if (m == m && found <= kList) {
+      by_rank<NT>(list, found, have, [&](int k, unsigned long long key) { best[k] = key; });
+    } else {
+      unsigned long long last = ~0ull;
+      for (int k = 0; k < have; ++k) {
+        unsigned long long high = 0;
+#pragma unroll
+        for (int q = 0; q < kVecs; ++q) {
+          if (q * NT + threadIdx.x < n) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
+              const unsigned long long key = top_key(x[q].get(e), v);
+              if (v >= 0 && v < a.V && key < last && key > high) high = key;
+            }
+          }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o);
+          high = other > high ? other : high;
+        }
+        __syncthreads();
+        if (lane == 0) list[warp] = high;
+        __syncthreads();
+        last = list[0];
+#pragma unroll
+        for (int q = 1; q < NW; ++q) last = list[q] > last ? list[q] : last;
+        if (threadIdx.x == 0) best[k] = last;
+      }
+    }
+  }
+  if (cluster == 1) {
+    __syncthreads();
+    const Stats t = part;
+    if (threadIdx.x == 0) write_row(a, row, r, t);
+    const float ls = log_sum(t);
+    for (int k = threadIdx.x; k < a.top; k += NT) {
+      const int v = key_token(best[k]);
+      a.top_id[(i64)r * a.top + k] = v;
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(row[v]), t, ls);
+    }
+    return;
+  }
+  // the first block joins what the others have found
+  cg::cluster_group all = cg::this_cluster();
+  all.sync();
+  if (rank == 0) {
+    Stats t = part;
+    for (int c = 1; c < cluster; ++c) t = joined(t, *all.map_shared_rank(&part, c));
+    int total = 0;
+    for (int c = 0; c < cluster; ++c) {        // (the same arithmetic as above tells how many each has)
+      const int clo = c * share, cn = max(0, min(at.vecs - clo, share));
+      const int cf = max(0, clo * E - at.skip), ce = min(a.V, (clo + cn) * E - at.skip), ch = min(a.top, max(0, ce - cf));
+      const unsigned long long* from = all.map_shared_rank(best, c);
+      for (int k = threadIdx.x; k < ch; k += NT) list[total + k] = from[k];
+      total += ch;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) write_row(a, row, r, t);
+    const float ls = log_sum(t);
+    by_rank<NT>(list, total, a.top, [&](int k, unsigned long long key) {
+      const int v = key_token(key);
+      a.top_id[(i64)r * a.top + k] = v;
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(row[v]), t, ls);
+    });
+  }
+  all.sync();                                  // nobody leaves while its shared memory may be read
+}
+
+// ---- log probabilities of short rows -----------------------------------------------------------------------------------------------
+
+// G lanes have a row, PER logits each
+template <int G> __device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o, G);
+  return v;
+}
+template <int G> __device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o, G));
+  return v;
+}
+constexpr int kShortThreads = 256;
+
+template <class T, int G, int PER>
+__global__ void __launch_bounds__(kShortThreads) logprob_short_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+  const int l = threadIdx.x % G;
+  pdl_wait();
+  pdl_trigger();
+  const i64 r_ = ((i64)blockIdx.x * kShortThreads + threadIdx.x) / G;
+  const bool live = r_ < a.N;
+  const int r = live ? (int)r_ : a.N - 1;      // (the last group's lanes go along)
+  const T* row = logits + (i64)r * a.ld;
+  float x[PER];
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = i * G + l < a.V ? to_f32(row[i * G + l]) : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) m = max_nan(m, x[i]);
+  m = group_max<G>(m);
+  const float m0 = ref_of(m);
+  Stats t{m, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float e = fmaxf((x[i] - m0) * kLog2e, -150.f), y = ex2(e);
+    t.s += y;
+    t.w = fmaf(y, e, t.w);
+  }
+  t.s = group_sum<G>(t.s);
+  t.w = group_sum<G>(t.w);
+  if (m == -INFINITY) t.s = t.w = 0.f;
+  if (l == 0 && live) write_row(a, row, r, t);
+  if (a.top == 0) return;
+  // the largest key, `top` times; a lane knows the largest of its own and looks for the next one when it is taken
+  const float ls = log_sum(t);
+  unsigned long long last = ~0ull;
+  for (int k = 0; k < a.top; ++k) {
+    unsigned long long high = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const unsigned long long key = top_key(x[i], i * G + l);
+      if (i * G + l < a.V && key < last && key > high) high = key;
+    }
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o, G);
+      high = other > high ? other : high;
+    }
+    last = high;
+    if (l == 0 && live) {
+      const int v = key_token(last);
+      const unsigned u = (unsigned)(last >> 32) ^ 0x80000000u;
+      a.top_id[(i64)r * a.top + k] = v;
+      a.top_logprob[(i64)r * a.top + k] = logprob_of((last >> 32) == 0u ? __int_as_float(0x7fc00000) : __uint_as_float((int)u < 0 ? u ^ 0x7fffffffu : u), t, ls);
+    }
+  }
+}
+
+// ---- log probabilities of rows beyond a cluster's registers -------------------------------------------------------------------------
+
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
 // sum of v over the block, the same bits in every thread
@@ -24,59 +399,39 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
 }
 __device__ __forceinline__ float block_max(float v, float* red) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
   __syncthreads();
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
   float s = red[0];
 #pragma unroll
-  for (int w = 1; w < kRowWarps; ++w) s = fmaxf(s, red[w]);
+  for (int w = 1; w < kRowWarps; ++w) s = max_nan(s, red[w]);
   return s;
 }
 
-// Order of the alternatives as one whole number: the value's bits so that they rise with the value (-0 as +0, NaN below -inf), then the
-// token, lower ones first.  Every key of a row is different and above zero.
-__device__ __forceinline__ unsigned long long top_key(float x, int v) {
-  x += 0.f;
-  const int b = __float_as_int(x);
-  const unsigned u = x != x ? 0u : (unsigned)(b < 0 ? b ^ 0x7fffffff : b) ^ 0x80000000u;
-  return ((unsigned long long)u << 32) | (unsigned)(0xffffffffu - (unsigned)v);
-}
-
-struct LogprobArgs {
-  int N, V, top; i64 ld;
-  const int32_t* tokens; float *logprob, *entropy, *lse, *top_logprob; int32_t* top_id;
-};
-
 template <class T>
-__global__ void __launch_bounds__(kRowThreads) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+__global__ void __launch_bounds__(kRowThreads) logprob_wide_kernel(const T* __restrict__ logits, const LogprobArgs a) {
   __shared__ float red[kRowWarps];
   __shared__ unsigned long long best[kRowWarps];
   const int r = blockIdx.x;
+  pdl_wait();
+  pdl_trigger();
   const T* x = logits + (i64)r * a.ld;
   float m = -INFINITY;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = fmaxf(m, to_f32(x[v]));
+  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = max_nan(m, to_f32(x[v]));
   m = block_max(m, red);
-  const float m0 = m == -INFINITY ? 0.f : m;
-  float s = 0.f, w = 0.f;
+  const float m0 = ref_of(m);
+  Stats t{m, 0.f, 0.f};
   for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-    const float d = to_f32(x[v]) - m0, e = expf(d);
-    s += e;
-    w += e == 0.f ? 0.f : e * d;
+    const float e = fmaxf((to_f32(x[v]) - m0) * kLog2e, -150.f), y = ex2(e);
+    t.s += y;
+    t.w = fmaf(y, e, t.w);
   }
-  s = block_sum(s, red);
-  w = block_sum(w, red);
-  // (log probabilities are (x - max) - log sum: x - lse would lose the second part where the row lies far from zero)
-  const float lse = s == 0.f ? -INFINITY : m0 + logf(s);
-  if (threadIdx.x == 0) {
-    if (a.lse) a.lse[r] = lse;
-    if (a.entropy) a.entropy[r] = s == 0.f ? 0.f : logf(s) - w / s;
-    if (a.tokens) {
-      const int t = a.tokens[r];
-      const float y = t >= 0 && t < a.V ? to_f32(x[t]) : 0.f;
-      a.logprob[r] = t >= 0 && t < a.V ? (s == 0.f ? -INFINITY : (y - m0) - logf(s)) : 0.f;
-    }
-  }
+  t.s = block_sum(t.s, red);
+  t.w = block_sum(t.w, red);
+  if (m == -INFINITY) t.s = t.w = 0.f;
+  if (threadIdx.x == 0) write_row(a, x, r, t);
+  const float ls = log_sum(t);
   unsigned long long last = ~0ull;
   for (int k = 0; k < a.top; ++k) {
     unsigned long long mine = 0;
@@ -95,41 +450,318 @@ __global__ void __launch_bounds__(kRowThreads) logprob_kernel(const T* __restric
     last = best[0];
     for (int q = 1; q < kRowWarps; ++q) last = best[q] > last ? best[q] : last;
     if (threadIdx.x == 0) {
-      const int v = (int)(0xffffffffu - (unsigned)last);
+      const int v = key_token(last);
       a.top_id[(i64)r * a.top + k] = v;
-      a.top_logprob[(i64)r * a.top + k] = s == 0.f ? -INFINITY : (to_f32(x[v]) - m0) - logf(s);
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(x[v]), t, ls);
     }
   }
 }
+
+// ---- gradient of log probabilities and entropies -----------------------------------------------------------------------------------
 
 struct LogprobGradArgs {
   int N, V; i64 ld, dld;
   const int32_t* tokens; const float *lse, *entropy, *dlogprob, *dentropy;
 };
+constexpr int kGradThreads = 256, kGradVecs = 4;
 
+// Statistics are given, so every element is on its own: a block has a part of a row, all of its loads in flight at once.
 template <class T>
-__global__ void __launch_bounds__(kRowThreads) logprob_back_kernel(const T* logits, T* dlogits, const LogprobGradArgs a) {
-  const int r = blockIdx.x;
-  const T* x = logits + (i64)r * a.ld;
-  T* d = dlogits + (i64)r * a.dld;
+__global__ void __launch_bounds__(kGradThreads) logprob_back_kernel(const T* logits, T* dlogits, const LogprobGradArgs a, int parts) {
+  constexpr int E = V16<T>::E;
+  const int r = blockIdx.x / parts, lo = (blockIdx.x - r * parts) * (kGradThreads * kGradVecs);
+  pdl_wait();
+  pdl_trigger();
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const RowAt<const T> at(row, a.V);
+  const RowAt<T> to(out, a.V);
+  V16<T> x[kGradVecs];
+#pragma unroll
+  for (int q = 0; q < kGradVecs; ++q) {
+    const int i = lo + q * kGradThreads + threadIdx.x;
+    if (i < at.vecs) x[q] = load_vec<T>(row, at, i, a.V);
+  }
   const int tok = a.tokens ? a.tokens[r] : -1;
   const bool has = tok >= 0 && tok < a.V;
   const float gl = has ? a.dlogprob[r] : 0.f, ge = a.dentropy ? a.dentropy[r] : 0.f, ent = a.dentropy ? a.entropy[r] : 0.f, lse = a.lse[r];
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-    const float logp = to_f32(x[v]) - lse, p = lse == -INFINITY ? 0.f : expf(logp);
-    float g = p == 0.f ? 0.f : -p * (gl + ge * (logp + ent));
-    if (v == tok && lse != -INFINITY) g += gl;
-    d[v] = from_f32<T>(g);
+  const bool dead = lse == -INFINITY;
+  const float c0 = fmaf(ge, ent, gl);          // gradient: -p (gl + ge (log p + ent)), and gl at the token
+#pragma unroll
+  for (int q = 0; q < kGradVecs; ++q) {
+    const int i = lo + q * kGradThreads + threadIdx.x;
+    if (i < at.vecs) {
+      V16<T> y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float logp = x[q].get(e) - lse, p = ex2(logp * kLog2e);
+        float g = p == 0.f ? 0.f : -p * fmaf(ge, logp, c0);
+        if (i * E + e - at.skip == tok) g += gl;
+        y.set(e, dead ? 0.f : g);
+      }
+      if (i > 0 && i + 1 < at.vecs && to.skip == at.skip) {
+        *(reinterpret_cast<uint4*>(to.base) + i) = y.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int v = i * E + e - at.skip;
+          if (v >= 0 && v < a.V) out[v] = y.raw(e);
+        }
+      }
+    }
   }
 }
 
+// ---- distillation --------------------------------------------------------------------------------------------------------------------
+
 struct DistillArgs {
   int N, V, K; i64 ld, dld; float tau;
-  const int32_t* top_id; const float *top_logit, *weight; float* row_loss;
+  const int32_t* top_id; const float *top_logit, *weight; float *row_loss, *loss;
 };
+// The student's side of one row: q = 2^((x - m) c) / s with c = log2(e) / tau
+struct Student { float m, s; };
 
+// A block, or a cluster, has a row in its registers (see above).  The gradient of the whole row is scale q; the places of the teacher's
+// alternatives are written once more, by the first of those that name the same token, after the block has written the rest.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
+  constexpr int E = V16<T>::E, NW = NT / 32;
+  __shared__ float prob[kMaxTeacher];          // teacher: logit / tau, then probability
+  __shared__ float gap[kMaxTeacher];           // student's logit
+  __shared__ int id[kMaxTeacher];
+  __shared__ float ra[NW], rb[NW], rc[NW];
+  __shared__ Student part;
+  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait();
+  pdl_trigger();
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const RowAt<const T> at(row, a.V);
+  const RowAt<T> to(out, a.V);
+  const int share = (at.vecs + cluster - 1) / cluster, lo = rank * share, n = max(0, min(at.vecs - lo, share));
+  V16<T> x[kVecs];
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q) {
+    const int i = q * NT + threadIdx.x;
+    if (i < n) x[q] = load_vec<T>(row, at, lo + i, a.V);
+  }
+  const float inv = 1.0f / a.tau, c = kLog2e * inv;
+  const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
+  // the teacher's alternatives, while the row is on its way
+  float ym = -INFINITY, any = 0.f;
+  for (int k = threadIdx.x; k < a.K; k += NT) {
+    const int v = a.top_id[(i64)r * a.K + k];
+    const bool in = v >= 0 && v < a.V;
+    const float y = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
+    id[k] = in ? v : -1;
+    prob[k] = y;
+    gap[k] = in ? to_f32(row[v]) : -INFINITY;
+    ym = fmaxf(ym, y);                         // (a NaN shows in the sum)
+    if (y != -INFINITY) any = 1.f;
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q)
+    if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
+  m = warp_max(m);
+  ym = warp_max(ym);
+  any = __any_sync(0xffffffffu, any != 0.f) ? 1.f : 0.f;
+  if (lane == 0) { ra[warp] = m; rb[warp] = ym; rc[warp] = any; }
+  __syncthreads();
+  m = ra[0];
+  ym = rb[0];
+  any = rc[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) { m = max_nan(m, ra[w]); ym = fmaxf(ym, rb[w]); any += rc[w]; }
+  __syncthreads();
+  const float m0 = ref_of(m), y0 = ref_of(ym);
+  float s = 0.f, mass = 0.f;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q) {
+    if (q * NT + threadIdx.x < n) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += ex2((x[q].get(e) - m0) * c);
+    }
+  }
+  for (int k = threadIdx.x; k < a.K; k += NT) mass += ex2((prob[k] - y0) * kLog2e);
+  s = warp_sum(s);
+  mass = warp_sum(mass);
+  if (lane == 0) { ra[warp] = s; rb[warp] = mass; }
+  __syncthreads();
+  s = mass = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { s += ra[w]; mass += rb[w]; }
+  float M = m0;
+  if (cluster > 1) {
+    cg::cluster_group all = cg::this_cluster();
+    if (threadIdx.x == 0) part = Student{m, s};
+    all.sync();                                // (also: every block has read what it needs before the first gradient is written)
+    Student each[kMaxCluster];
+    M = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q) {
+      if (q < cluster) {
+        each[q] = *all.map_shared_rank(&part, q);
+        M = max_nan(M, each[q].m);
+      }
+    }
+    all.barrier_arrive();                      // (waited for at the end: nobody leaves while its shared memory may be read)
+    M = ref_of(M);
+    s = 0.f;
+#pragma unroll
+    for (int q = 0; q < kMaxCluster; ++q)
+      if (q < cluster) s += each[q].s == 0.f ? 0.f : each[q].s * ex2((each[q].m - M) * c);
+  }
+  const float ls = logf(s), lmass = logf(mass), scale = weight * a.tau;
+  float loss = 0.f;
+  for (int k = threadIdx.x; k < a.K; k += NT) {
+    const float logp = (prob[k] - y0) - lmass, p = ex2(logp * kLog2e), z = gap[k];
+    const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
+    loss += p == 0.f ? 0.f : p * (logp - logq);
+    prob[k] = p;
+  }
+  if (rank == 0) {
+    loss = warp_sum(loss);
+    if (lane == 0) rc[warp] = loss;
+  }
+  const bool none = any == 0.f || weight == 0.f;
+  const float f = none || s == 0.f ? 0.f : scale / s;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q) {
+    const int j = q * NT + threadIdx.x, i = lo + j;
+    if (j < n) {
+      V16<T> y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float g = ex2((x[q].get(e) - M) * c) * f;
+        y.set(e, none ? 0.f : g);
+      }
+      if (i > 0 && i + 1 < at.vecs && to.skip == at.skip) {
+        __stcs(reinterpret_cast<uint4*>(to.base) + i, y.w);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int v = i * E + e - at.skip;
+          if (v >= 0 && v < a.V) out[v] = y.raw(e);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (rank == 0 && threadIdx.x == 0) {
+    float t = 0.f;
+    for (int w = 0; w < NW; ++w) t += rc[w];
+    a.row_loss[r] = any != 0.f ? a.tau * a.tau * t : 0.f;
+  }
+  if (!none) {
+    const int first = lo * E - at.skip, end = (lo + n) * E - at.skip;      // the block's own tokens
+    for (int k = threadIdx.x; k < a.K; k += NT) {
+      const int v = id[k];
+      if (v < 0 || v < first || v >= end) continue;
+      float p = 0.f;
+      bool again = false;
+      for (int j = 0; j < a.K; ++j) {
+        if (id[j] != v) continue;
+        again = again || j < k;
+        p += prob[j];
+      }
+      if (again) continue;
+      const float q = s == 0.f ? 0.f : ex2((gap[k] - M) * c) / s;
+      out[v] = from_f32<T>(scale * (q - p));
+    }
+  }
+  if (cluster > 1) cg::this_cluster().barrier_wait();
+}
+
+// Short rows: G lanes have a row, PER logits each; the teacher's probabilities of each token meet in shared memory, in the order of the
+// alternatives.
+template <class T, int G, int PER>
+__global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+  constexpr int ROWS = kShortThreads / G;
+  __shared__ float target[ROWS][G * PER];
+  __shared__ float part[ROWS];
+  const int l = threadIdx.x % G, g = threadIdx.x / G;
+  pdl_wait();
+  pdl_trigger();
+  const i64 r_ = (i64)blockIdx.x * ROWS + g;
+  const bool live = r_ < a.N;
+  const int r = live ? (int)r_ : a.N - 1;
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const float inv = 1.0f / a.tau, c = kLog2e * inv;
+  const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
+  const int32_t* ids = a.top_id + (i64)r * a.K;
+  const float* ys = a.top_logit + (i64)r * a.K;
+  float x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = i * G + l < a.V ? to_f32(row[i * G + l]) : -INFINITY;
+  float m = -INFINITY, s = 0.f, ym = -INFINITY, mass = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) { m = max_nan(m, x[i]); target[g][i * G + l] = 0.f; }
+  m = group_max<G>(m);
+  const float M = ref_of(m);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) s += ex2((x[i] - M) * c);
+  s = group_sum<G>(s);
+  const auto teacher = [&](int k) {
+    const int v = k < a.K ? ids[k] : -1;
+    return v >= 0 && v < a.V ? ys[k] * inv : -INFINITY;
+  };
+  float any = 0.f;
+  for (int k = l; k < a.K; k += G) {
+    const float y = teacher(k);
+    ym = fmaxf(ym, y);
+    if (y != -INFINITY) any = 1.f;
+  }
+  ym = group_max<G>(ym);
+  any = group_max<G>(any);
+  const float y0 = ref_of(ym);
+  for (int k = l; k < a.K; k += G) mass += ex2((teacher(k) - y0) * kLog2e);
+  mass = group_sum<G>(mass);
+  const float ls = logf(s), lmass = logf(mass);
+  float loss = 0.f;
+  __syncwarp();
+  for (int k0 = 0; k0 < a.K; k0 += G) {
+    const int k = k0 + l, v = k < a.K ? ids[k] : -1;
+    const bool in = v >= 0 && v < a.V;
+    float p = 0.f;
+    if (in) {
+      const float logp = (ys[k] * inv - y0) - lmass, z = to_f32(row[v]);
+      const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
+      p = ex2(logp * kLog2e);
+      loss += p == 0.f ? 0.f : p * (logp - logq);
+    }
+    for (int j = 0; j < G; ++j) {              // (the lane that owns a token adds to it)
+      const int w = __shfl_sync(0xffffffffu, in ? v : -1, j, G);
+      const float pw = __shfl_sync(0xffffffffu, p, j, G);
+      if (w >= 0 && w % G == l) target[g][w] += pw;
+    }
+  }
+  loss = group_sum<G>(loss);
+  loss = any != 0.f ? a.tau * a.tau * loss : 0.f;
+  if (l == 0 && live) a.row_loss[r] = loss;
+  const bool none = any == 0.f || weight == 0.f;
+  const float scale = weight * a.tau, f = s == 0.f ? 0.f : 1.0f / s;
+  __syncwarp();                                // every lane of the row has read it
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float q = s == 0.f ? 0.f : ex2((x[i] - M) * c) * f;
+    if (live && i * G + l < a.V) out[i * G + l] = from_f32<T>(none ? 0.f : scale * (q - target[g][i * G + l]));
+  }
+  if (gridDim.x == 1) {                        // the only block also adds the rows' losses up
+    if (l == 0) part[g] = live && weight != 0.f ? weight * loss : 0.f;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      float t = threadIdx.x < ROWS ? part[threadIdx.x] : 0.f;
+      t = warp_sum(t);
+      if (threadIdx.x == 0) *a.loss = t;
+    }
+  }
+}
+
+// rows beyond a cluster's registers
 template <class T>
-__global__ void __launch_bounds__(kRowThreads) distill_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+__global__ void __launch_bounds__(kRowThreads) distill_wide_kernel(const T* logits, T* dlogits, const DistillArgs a) {
   __shared__ float red[kRowWarps];
   __shared__ float prob[kMaxTeacher];
   __shared__ int id[kMaxTeacher];
@@ -138,6 +770,8 @@ __global__ void __launch_bounds__(kRowThreads) distill_kernel(const T* logits, T
   const T* x = logits + (i64)r * a.ld;
   T* d = dlogits + (i64)r * a.dld;
   const float inv = 1.0f / a.tau;
+  pdl_wait();
+  pdl_trigger();
   // the teacher
   float ym = -INFINITY, present = 0.f;
   for (int k = threadIdx.x; k < a.K; k += kRowThreads) {
@@ -147,7 +781,7 @@ __global__ void __launch_bounds__(kRowThreads) distill_kernel(const T* logits, T
     id[k] = in ? v : -1;
     prob[k] = y;
     logit[k] = in ? to_f32(x[v]) * inv : -INFINITY;
-    ym = fmaxf(ym, y);
+    ym = fmaxf(ym, y);      // (a NaN shows in the sum)
     if (y != -INFINITY) present = 1.f;
   }
   present = block_sum(present, red);
@@ -159,7 +793,7 @@ __global__ void __launch_bounds__(kRowThreads) distill_kernel(const T* logits, T
   mass = block_sum(mass, red);
   // the student
   float m = -INFINITY;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = fmaxf(m, to_f32(x[v]) * inv);
+  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = max_nan(m, to_f32(x[v]) * inv);
   m = block_max(m, red);
   if (m == -INFINITY) m = 0.f;
   float s = 0.f;
@@ -178,16 +812,27 @@ __global__ void __launch_bounds__(kRowThreads) distill_kernel(const T* logits, T
   const float scale = w * a.tau;
   const bool none = present == 0.f || w == 0.f;
   for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-    const float e = expf(to_f32(x[v]) * inv - m);
-    float q = s == 0.f ? 0.f : e / s;
-    for (int k = 0; k < a.K; ++k)
-      if (id[k] == v) q -= prob[k];
+    const float q = s == 0.f ? 0.f : expf(to_f32(x[v]) * inv - m) / s;
     d[v] = from_f32<T>(none ? 0.f : scale * q);
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < a.K && !none; k += kRowThreads) {
+    const int v = id[k];
+    if (v < 0) continue;
+    float p = 0.f;
+    bool again = false;
+    for (int j = 0; j < a.K; ++j) {
+      if (id[j] != v) continue;
+      again = again || j < k;
+      p += prob[j];
+    }
+    if (!again) d[v] = from_f32<T>(scale * ((s == 0.f ? 0.f : expf(logit[k] - m) / s) - p));
   }
 }
 
 __global__ void __launch_bounds__(1024) distill_loss_kernel(int N, const float* __restrict__ row_loss, const float* __restrict__ weight, float* __restrict__ loss) {
   __shared__ float part[32];
+  pdl_wait();
   float s = 0.f;
   for (int r = threadIdx.x; r < N; r += 1024) {
     const float w = weight ? weight[r] : 1.0f / (float)N;
@@ -210,7 +855,36 @@ int check_logits(int N, int V, int dtype, const void* logits, i64 ld) {
   if (N == 0) return MGRIT_OK;
   return !logits || !elem_aligned(logits, dtype) || (N > 1 && ld < V) ? MGRIT_INVALID_ARG : MGRIT_OK;
 }
-int launched() { return cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR; }
+int launched(cudaError_t e) {
+  count_launch();
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
+}
+
+// Blocks that share a row of `vecs` vectors, and their threads.  The fewest that hold it, 128 threads where they suffice; where that leaves
+// SMs without work, more of them, down to two vectors a thread (8 rows of 131072 in bf16: 21 us on 32 blocks, 9 on 128).  0: too long.
+struct Split { int cluster, threads; };
+Split split_of(int N, i64 vecs) {
+  const i64 whole = 512 * kVecs;
+  if (vecs > kMaxCluster * whole) return {0, 0};
+  if (vecs <= 128 * kVecs && (i64)N * ((vecs + 255) / 256) >= 296) return {1, 128};
+  int c = 1;
+  while ((vecs + c - 1) / c > whole) c *= 2;
+  while (c < kMaxCluster && (i64)N * c < 148 && vecs / (2 * c) >= 1024) c *= 2;
+  return {c, 512};
+}
+template <class... KArgs, class... Args>
+cudaError_t launch_rows(void (*kern)(KArgs...), int N, Split sp, cudaStream_t s, Args&&... args) {
+  if (sp.cluster > 8) {                        // more than the portable size
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl_cluster(kern, sp.cluster, dim3((unsigned)N * sp.cluster), dim3(sp.threads), 0, s, static_cast<Args&&>(args)..., sp.cluster);
+}
+// vectors of a row; one more where rows start inside a vector
+i64 vecs_of(int V, int dtype, const void* p, i64 ld) {
+  const i64 es = (i64)elem_size(dtype);
+  return (V * es + 15) / 16 + ((((uintptr_t)p | (uintptr_t)(ld * es)) & 15u) ? 1 : 0);
+}
 
 }  // namespace
 }  // namespace mg
@@ -226,13 +900,22 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
   if (!aligned4(tokens) || !aligned4(logprob) || !aligned4(entropy) || !aligned4(lse) || !aligned4(top_logprob) || !aligned4(top_id)) return MGRIT_INVALID_ARG;
   if (top > kMaxTop) return MGRIT_UNSUPPORTED;
   if (N == 0) return MGRIT_OK;
+  cudaError_t e = cudaSuccess;
   const LogprobArgs a{N, V, top, ld, tokens, logprob, entropy, lse, top_logprob, top_id};
   with_elem(dtype, [&](auto tag) {
     using T = decltype(tag);
-    logprob_kernel<T><<<N, kRowThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(logits), a);
+    const T* x = static_cast<const T*>(logits);
+    cudaStream_t s = (cudaStream_t)stream;
+    const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
+    const auto few = [&](auto kern, int lanes) { e = launch_pdl(kern, dim3((unsigned)(((i64)N * lanes + kShortThreads - 1) / kShortThreads)), dim3(kShortThreads), 0, s, x, a); };
+    if (V <= 64) few(logprob_short_kernel<T, 8, 8>, 8);
+    else if (V <= 256) few(logprob_short_kernel<T, 32, 8>, 32);
+    else if (V <= kShortRow) few(logprob_short_kernel<T, 32, 32>, 32);
+    else if (sp.cluster == 0) e = launch_pdl(logprob_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, a);
+    else if (sp.threads == 128) e = launch_rows(logprob_kernel<T, 128>, N, sp, s, x, a);
+    else e = launch_rows(logprob_kernel<T, 512>, N, sp, s, x, a);
   });
-  count_launch();
-  return launched();
+  return launched(e);
 }
 
 int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* logits, int64_t ld, const int32_t* tokens,
@@ -246,13 +929,16 @@ int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* log
   if (N == 0) return MGRIT_OK;
   if (!lse || !tokens != !dlogprob || !entropy != !dentropy || (!tokens && !entropy)) return MGRIT_INVALID_ARG;
   if (dlogits == logits && dld != ld && N > 1) return MGRIT_INVALID_ARG;
+  const i64 parts = (vecs_of(V, dtype, logits, ld) + kGradThreads * kGradVecs - 1) / (kGradThreads * kGradVecs);
+  if (N * parts >= INT32_MAX) return MGRIT_UNSUPPORTED;
+  cudaError_t e = cudaSuccess;
   const LogprobGradArgs a{N, V, ld, dld, tokens, lse, entropy, dlogprob, dentropy};
   with_elem(dtype, [&](auto tag) {
     using T = decltype(tag);
-    logprob_back_kernel<T><<<N, kRowThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(logits), static_cast<T*>(dlogits), a);
+    e = launch_pdl(logprob_back_kernel<T>, dim3((unsigned)(N * parts)), dim3(kGradThreads), 0, (cudaStream_t)stream, static_cast<const T*>(logits), static_cast<T*>(dlogits), a,
+                   (int)parts);
   });
-  count_launch();
-  return launched();
+  return launched(e);
 }
 
 int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float tau, const void* logits, int64_t ld,
@@ -268,16 +954,30 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
   if (N > 0) {
     if (!top_id || !top_logit || !row_loss || (dlogits == logits && dld != ld && N > 1)) return MGRIT_INVALID_ARG;
     if (!aligned4(top_id) || !aligned4(top_logit) || !aligned4(weight) || !aligned4(row_loss)) return MGRIT_INVALID_ARG;
-    const DistillArgs a{N, V, K, ld, dld, tau, top_id, top_logit, weight, row_loss};
+    const DistillArgs a{N, V, K, ld, dld, tau, top_id, top_logit, weight, row_loss, loss};
+    cudaError_t e = cudaSuccess;
+    bool added = false;
     with_elem(dtype, [&](auto tag) {
       using T = decltype(tag);
-      distill_kernel<T><<<N, kRowThreads, 0, s>>>(static_cast<const T*>(logits), static_cast<T*>(dlogits), a);
+      const T* x = static_cast<const T*>(logits);
+      T* d = static_cast<T*>(dlogits);
+      const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
+      const auto few = [&](auto kern, int lanes) {
+        const i64 blocks = ((i64)N * lanes + kShortThreads - 1) / kShortThreads;
+        added = blocks == 1;
+        e = launch_pdl(kern, dim3((unsigned)blocks), dim3(kShortThreads), 0, s, x, d, a);
+      };
+      if (V <= 64) few(distill_short_kernel<T, 8, 8>, 8);
+      else if (V <= 256) few(distill_short_kernel<T, 32, 8>, 32);
+      else if (V <= kShortRow) few(distill_short_kernel<T, 32, 32>, 32);
+      else if (sp.cluster == 0) e = launch_pdl(distill_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, d, a);
+      else if (sp.threads == 128) e = launch_rows(distill_kernel<T, 128>, N, sp, s, x, d, a);
+      else e = launch_rows(distill_kernel<T, 512>, N, sp, s, x, d, a);
     });
-    count_launch();
+    rc = launched(e);
+    if (rc != MGRIT_OK || added) return rc;
   }
-  distill_loss_kernel<<<1, 1024, 0, s>>>(N, row_loss, weight, loss);
-  count_launch();
-  return launched();
+  return launched(launch_pdl(distill_loss_kernel, dim3(1), dim3(1024), 0, s, N, (const float*)row_loss, weight, loss));
 }
 
 }  // extern "C"
