@@ -5,7 +5,7 @@
 // quarters of that time (16 a cycle and SM).  Rows of up to 16 x kThreads x kVecs vectors are held in registers:
 //  * short rows (V <= 1024): a group of 8 or 32 lanes has a row;
 //  * longer ones: a block, or a cluster of up to 16 blocks that share a row and meet through distributed shared memory.  A thread
-//    loads all of its 16-byte vectors at once, so that the largest logit, the sums, the top alternatives and the gradient are all
+//    loads all of its 16-byte vectors at once, the next row's while it works on one, so that the largest logit, the sums, the top alternatives and the gradient are all
 //    formed without reading a row again, and without the rescaling that running sums need.  Few rows are split over more blocks than
 //    they need, so that a single token's row of 131072 is read by 16 SMs;
 //  * rows beyond that: a block per row in several passes (only their first one from HBM, the others mostly from L2).
@@ -21,12 +21,11 @@ namespace mg {
 namespace {
 
 constexpr int kMaxTop = 128, kMaxTeacher = 1024;
-constexpr int kVecs = 8;                       // 16-byte vectors of a thread
+constexpr int kVecs = 16;                      // 16-byte vectors of a thread
 constexpr int kMaxCluster = 16;
 constexpr int kShortRow = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
 // Order of the alternatives as one whole number: the value's bits so that they rise with the value (-0 as +0, NaN below -inf), then the
@@ -37,6 +36,7 @@ __device__ __forceinline__ unsigned value_key(float x) {
   return x != x ? 0u : (unsigned)(b < 0 ? b ^ 0x7fffffff : b) ^ 0x80000000u;
 }
 __device__ __forceinline__ unsigned long long top_key(float x, int v) { return ((unsigned long long)value_key(x) << 32) | (unsigned)(0xffffffffu - (unsigned)v); }
+__device__ __forceinline__ float key_value(unsigned k) { const unsigned u = k ^ 0x80000000u; return k == 0u ? __int_as_float(0x7fc00000) : __uint_as_float((int)u < 0 ? u ^ 0x7fffffffu : u); }
 __device__ __forceinline__ int key_token(unsigned long long k) { return (int)(0xffffffffu - (unsigned)k); }
 
 // ---- vectors of 16 bytes ---------------------------------------------------------------------------------------------------------
@@ -47,6 +47,25 @@ template <class T> struct V16 {
   __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(&w)[i]); }
   __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&w)[i] = from_f32<T>(v); }
   __device__ __forceinline__ T& raw(int i) { return reinterpret_cast<T*>(&w)[i]; }
+  // elements 2 i and 2 i + 1
+  __device__ __forceinline__ F<2> pair(int i) const {
+    const unsigned* u = reinterpret_cast<const unsigned*>(&w);
+    if constexpr (sizeof(T) == 4) {
+      return F<2>{{__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1])}};
+    } else {
+      const float2 f = unpack2(u[i], T{});
+      return F<2>{{f.x, f.y}};
+    }
+  }
+  __device__ __forceinline__ void set_pair(int i, const F<2>& f) {
+    unsigned* u = reinterpret_cast<unsigned*>(&w);
+    if constexpr (sizeof(T) == 4) {
+      u[2 * i] = __float_as_uint(f.x[0]);
+      u[2 * i + 1] = __float_as_uint(f.x[1]);
+    } else {
+      u[i] = pack2(f.x[0], f.x[1], T{});
+    }
+  }
 };
 // the largest element, NaN where there is one (two 16-bit values an instruction)
 __device__ __forceinline__ unsigned max2(unsigned a, unsigned b, __nv_bfloat16) { unsigned y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b)); return y; }
@@ -86,6 +105,65 @@ template <class T> __device__ __forceinline__ V16<T> load_vec(const T* row, cons
   return v;
 }
 
+// A block's share of a row on its way to registers: a thread copies its vectors to its own places in shared memory, asynchronously, while the
+// row before is worked on, and reads them back itself, so nobody waits for anybody.  Vectors at a row's ends are copied whole where the
+// bytes around the row belong to the array (they are replaced by -inf when read back), and element by element where they do not.
+template <class T, int NT> struct Stage {
+  static constexpr int E = V16<T>::E;
+  const T *first, *end;                        // the array
+  i64 ld;
+  int V, cluster, rank;
+  uint4* mine;                                 // the thread's places, NT apart
+  __device__ __forceinline__ int share(const RowAt<const T>& at) const { return (at.vecs + cluster - 1) / cluster; }
+  __device__ __forceinline__ void bring(i64 r) const {
+    const T* row = first + r * ld;
+    const RowAt<const T> at(row, V);
+    const int per = share(at), lo = rank * per, n = max(0, min(at.vecs - lo, per));
+    const T* p = at.base + (i64)(lo + (int)threadIdx.x) * E;
+    const unsigned to = (unsigned)__cvta_generic_to_shared(mine);
+    // all but the array's own ends, where a vector would reach outside
+    const bool cut_head = lo == 0 && at.base < first, cut_tail = n > 0 && at.base + (i64)(lo + n) * E > end;
+    const int left = n - (cut_tail ? 1 : 0) - (int)threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q)
+      if (q * NT < left && !(q == 0 && cut_head && threadIdx.x == 0))
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + q * (NT * 16)), "l"(p + q * (NT * E)) : "memory");
+    if (cut_head || cut_tail) {
+#pragma unroll 1
+      for (int q = 0; q < kVecs; ++q) {
+        const int i = q * NT + (int)threadIdx.x;
+        if ((cut_head && i == 0) || (cut_tail && i == n - 1)) {
+#pragma unroll 1
+          for (int e = 0; e < E; ++e) {
+            const T* from = p + (i64)q * (NT * E) + e;
+            if (from >= first && from < end) reinterpret_cast<T*>(mine + q * NT)[e] = *from;
+          }
+        }
+      }
+    }
+  }
+  // -> the number of the block's vectors, and where they start in the row
+  __device__ __forceinline__ int take(i64 r, V16<T> (&x)[kVecs], int& lo) const {
+    const RowAt<const T> at(first + r * ld, V);
+    const int per = share(at);
+    lo = rank * per;
+    const int n = max(0, min(at.vecs - lo, per));
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (lo == 0 && threadIdx.x == 0)
+#pragma unroll 1
+      for (int e = 0; e < at.skip; ++e) reinterpret_cast<T*>(mine)[e] = from_f32<T>(-INFINITY);
+    const int last = at.vecs - 1 - lo;         // the row's last vector, counted from the block's first
+    if (last >= 0 && last < n && last % NT == (int)threadIdx.x)
+#pragma unroll 1
+      for (int e = V + at.skip - (at.vecs - 1) * E; e < E; ++e) reinterpret_cast<T*>(mine + last / NT * NT)[e] = from_f32<T>(-INFINITY);
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q)
+      if (q * NT < n - (int)threadIdx.x) x[q].w = mine[q * NT];
+    return n;
+  }
+};
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
 // ---- reductions over a block -----------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -98,6 +176,10 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
+
+// what the warps of a block have left, one value each: every warp puts them together for itself
+template <int NW> __device__ __forceinline__ float all_max(const float* v) { const int l = threadIdx.x & 31; return warp_max(l < NW ? v[l] : -INFINITY); }
+template <int NW> __device__ __forceinline__ float all_sum(const float* v) { const int l = threadIdx.x & 31; return warp_sum(l < NW ? v[l] : 0.f); }
 
 // Statistics of some of a row's logits: the largest, m; s = sum 2^((x - m) log2 e); w = sum of the same terms times their exponents.
 // A part without any logit above -inf has m = -inf and s = 0.
@@ -141,6 +223,7 @@ template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsig
   for (int i = threadIdx.x; i < n; i += NT) {
     const unsigned long long k = list[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) rank += list[j] > k;
     if (rank < top) out(rank, k);
   }
@@ -151,165 +234,171 @@ template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsig
 // those that do are few (some hundred of 32768 random ones for top = 20); they are put in order by counting.  Where ties or a NaN
 // make them many, the largest is taken out `top` times instead.
 template <class T, int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
+__global__ void __launch_bounds__(NT, 512 / NT) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
   constexpr int E = V16<T>::E, NW = NT / 32;
+  extern __shared__ uint4 staged[];
   __shared__ unsigned long long list[kList];
-  __shared__ unsigned long long best[kMaxTop];
+  __shared__ unsigned long long best[2][kMaxTop];
   __shared__ float wmax[NW], wbound[NW], wsum[NW], wdot[NW];
-  __shared__ Stats part;
-  __shared__ int count;
-  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ Stats part[2];
+  __shared__ int count[2];
+  const int rank = blockIdx.x % cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.x / cluster;
   pdl_wait();
   pdl_trigger();
-  const T* row = logits + (i64)r * a.ld;
-  const RowAt<const T> at(row, a.V);
-  const int share = (at.vecs + cluster - 1) / cluster, lo = rank * share, n = max(0, min(at.vecs - lo, share));      // the block's vectors
-  V16<T> x[kVecs];
+  const Stage<T, NT> stage{logits, logits + ((i64)(a.N - 1) * a.ld + a.V), a.ld, a.V, cluster, rank, staged + threadIdx.x};
+  int r = blockIdx.x / cluster;
+  if (r < a.N) stage.bring(r);
+  copies_issued();
+  if (threadIdx.x < 2) count[threadIdx.x] = 0;
+  for (int buf = 0; r < a.N; r += step, buf ^= 1) {
+    V16<T> x[kVecs];
+    int lo;
+    const int n = stage.take(r, x, lo);        // the block's vectors
+    if (r + step < a.N) stage.bring(r + step);
+    copies_issued();
+    const T* row = logits + (i64)r * a.ld;
+    const RowAt<const T> at(row, a.V);
+    float m = -INFINITY;
 #pragma unroll
-  for (int q = 0; q < kVecs; ++q) {
-    const int i = q * NT + threadIdx.x;
-    if (i < n) x[q] = load_vec<T>(row, at, lo + i, a.V);
-  }
-  if (threadIdx.x == 0) count = 0;
-  float m = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q)
-    if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
-  const float mine = m;
-  m = warp_max(m);
-  if (lane == 0) wmax[warp] = m;
-  if (a.top > 0) {
-    // the warp's j-th largest of its lanes' largest logits; warps without logits have no say
-    const int warps = min(NW, (n + 31) / 32), j = (a.top + max(warps, 1) - 1) / max(warps, 1);
-    unsigned k = value_key(mine), b = 0u;
-    for (int i = 0; i < min(j, 32); ++i) {
-      b = __reduce_max_sync(0xffffffffu, k);
-      const unsigned who = __ballot_sync(0xffffffffu, k == b);
-      if (lane == __ffs(who) - 1) k = 0u;
-    }
-    if (j > 32) b = 0u;
-    const unsigned u = b ^ 0x80000000u;
-    if (lane == 0) wbound[warp] = warp * 32 < n ? (b == 0u ? -INFINITY : __uint_as_float((int)u < 0 ? u ^ 0x7fffffffu : u)) : INFINITY;
-  }
-  __syncthreads();
-  m = wmax[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) m = max_nan(m, wmax[w]);
-  // sums: exponents stop at -150, where the terms are zero (a term of -inf would make 0 x inf of its product)
-  const float m0 = ref_of(m);
-  float s = 0.f, w = 0.f;
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q) {
-    if (q * NT + threadIdx.x < n) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float t = fmaxf((x[q].get(e) - m0) * kLog2e, -150.f), y = ex2(t);
-        s += y;
-        w = fmaf(y, t, w);
+    for (int q = 0; q < kVecs; ++q)
+      if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
+    const float mine = m;
+    m = warp_max(m);
+    if (lane == 0) wmax[warp] = m;
+    if (a.top > 0) {
+      // the warp's j-th largest of its lanes' largest logits; warps without logits have no say
+      const int warps = max(1, min(NW, (n + 31) / 32)), j = (a.top + warps - 1) / warps;
+      unsigned k = value_key(mine), b = 0u;
+      for (int i = 0; i < min(j, 32); ++i) {
+        b = __reduce_max_sync(0xffffffffu, k);
+        const unsigned who = __ballot_sync(0xffffffffu, k == b);
+        if (lane == __ffs(who) - 1) k = 0u;
       }
+      if (j > 32) b = 0u;
+      if (lane == 0) wbound[warp] = warp * 32 < n ? (b == 0u ? INFINITY : -key_value(b)) : -INFINITY;
     }
-  }
-  s = warp_sum(s);
-  w = warp_sum(w);
-  if (lane == 0) { wsum[warp] = s; wdot[warp] = w; }
-  float bound = INFINITY;
-  if (a.top > 0) {
+    __syncthreads();
+    m = all_max<NW>(wmax);
+    // sums: exponents stop at -150, where the terms are zero (a term of -inf would make 0 x inf of its product)
+    const float m0 = ref_of(m);
+    F<2> s = F<2>::all(0.f), w = F<2>::all(0.f);
+    const F<2> from = F<2>::all(-m0), scale = F<2>::all(kLog2e);
 #pragma unroll
-    for (int q = 0; q < NW; ++q) bound = fminf(bound, wbound[q]);
-    if (mine >= bound) {
+    for (int q = 0; q < kVecs; ++q) {
+      if (q * NT + threadIdx.x < n) {
 #pragma unroll
-      for (int q = 0; q < kVecs; ++q) {
-        if (q * NT + threadIdx.x < n && max_of(x[q]) >= bound) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
-            if (x[q].get(e) >= bound && v >= 0 && v < a.V) {
-              const int at_ = atomicAdd(&count, 1);
-              if (at_ < kList) list[at_] = top_key(x[q].get(e), v);
-            }
-          }
+        for (int e = 0; e < E / 2; ++e) {
+          const F<2> t = each((x[q].pair(e) + from) * scale, [](float v, int) { return fmaxf(v, -150.f); });
+          const F<2> y = each(t, [](float v, int) { return ex2(v); });
+          s = s + y;
+          w = fma_(y, t, w);
         }
       }
     }
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    Stats t{m, 0.f, 0.f};
-    for (int q = 0; q < NW; ++q) { t.s += wsum[q]; t.w += wdot[q]; }
-    if (m == -INFINITY) t.s = t.w = 0.f;
-    part = t;
-  }
-  const int first = max(0, lo * E - at.skip), end = min(a.V, (lo + n) * E - at.skip), have = min(a.top, max(0, end - first));      // the block's own best
-  if (a.top > 0) {
-    const int found = count;
-    if (m == m && found <= kList) {
-      by_rank<NT>(list, found, have, [&](int k, unsigned long long key) { best[k] = key; });
-    } else {
-      unsigned long long last = ~0ull;
-      for (int k = 0; k < have; ++k) {
-        unsigned long long high = 0;
+    const float s1 = warp_sum(s.x[0] + s.x[1]), w1 = warp_sum(w.x[0] + w.x[1]);
+    if (lane == 0) { wsum[warp] = s1; wdot[warp] = w1; }
+    if (threadIdx.x == 0) count[buf ^ 1] = 0;
+    if (a.top > 0) {
+      const float bound = -all_max<NW>(wbound);      // (they are kept with their signs turned)
+      if (mine >= bound) {
 #pragma unroll
         for (int q = 0; q < kVecs; ++q) {
-          if (q * NT + threadIdx.x < n) {
+          if (q * NT + threadIdx.x < n && max_of(x[q]) >= bound) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
               const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
-              const unsigned long long key = top_key(x[q].get(e), v);
-              if (v >= 0 && v < a.V && key < last && key > high) high = key;
+              if (x[q].get(e) >= bound && v >= 0 && v < a.V) {
+                const int place = atomicAdd(&count[buf], 1);
+                if (place < kList) list[place] = top_key(x[q].get(e), v);
+              }
             }
           }
         }
+      }
+    }
+    __syncthreads();
+    Stats t{m, 0.f, 0.f};
+    t.s = all_sum<NW>(wsum);
+    t.w = all_sum<NW>(wdot);
+    if (m == -INFINITY) t.s = t.w = 0.f;
+    const auto answer = [&](int k, unsigned long long key, const Stats& t, float ls) {
+      a.top_id[(i64)r * a.top + k] = key_token(key);
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value((unsigned)(key >> 32)), t, ls);
+    };
+    const float ls = log_sum(t);
+    if (threadIdx.x == 0) {
+      if (cluster == 1) write_row(a, row, r, t);
+      else part[buf] = t;
+    }
+    const auto own = [&](int c) {              // how many alternatives block c of the cluster can have
+      const int per = (at.vecs + cluster - 1) / cluster, l = c * per, h = min(at.vecs, l + per);
+      return min(a.top, max(0, min(a.V, h * E - at.skip) - max(0, l * E - at.skip)));
+    };
+    if (a.top > 0) {
+      const int have = own(rank), found = count[buf];
+      const auto keep = [&](int k, unsigned long long key) {
+        if (cluster == 1) answer(k, key, t, ls);
+        else best[buf][k] = key;
+      };
+      if (m == m && found <= kList) {
+        by_rank<NT>(list, found, have, keep);
+      } else {
+        unsigned long long last = ~0ull;
+        for (int k = 0; k < have; ++k) {
+          unsigned long long high = 0;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o);
-          high = other > high ? other : high;
+          for (int q = 0; q < kVecs; ++q) {
+            if (q * NT + threadIdx.x < n) {
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
+                const unsigned long long key = top_key(x[q].get(e), v);
+                if (v >= 0 && v < a.V && key < last && key > high) high = key;
+              }
+            }
+          }
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o);
+            high = other > high ? other : high;
+          }
+          __syncthreads();
+          if (lane == 0) list[warp] = high;
+          __syncthreads();
+          last = list[0];
+#pragma unroll
+          for (int q = 1; q < NW; ++q) last = list[q] > last ? list[q] : last;
+          if (threadIdx.x == 0) keep(k, last);
+        }
+      }
+    }
+    if (cluster > 1) {
+      // the first block joins what the others have found, while they go on to the next row
+      cg::cluster_group all = cg::this_cluster();
+      all.sync();
+      if (rank == 0) {
+        // a lane fetches a block's statistics, a thread one alternative: one trip to the other blocks, not one for each
+        t = lane < cluster ? *all.map_shared_rank(&part[buf], lane) : Stats{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+          const Stats b{__shfl_down_sync(0xffffffffu, t.m, o), __shfl_down_sync(0xffffffffu, t.s, o), __shfl_down_sync(0xffffffffu, t.w, o)};
+          t = joined(t, b);
+        }
+        t = Stats{__shfl_sync(0xffffffffu, t.m, 0), __shfl_sync(0xffffffffu, t.s, 0), __shfl_sync(0xffffffffu, t.w, 0)};
+        // (places without an alternative hold zero, below every key)
+        const int total = cluster * a.top;
+        for (int k = threadIdx.x; k < total; k += NT) {
+          const int c = k / a.top;
+          list[k] = k - c * a.top < own(c) ? all.map_shared_rank(best[buf], c)[k - c * a.top] : 0ull;
         }
         __syncthreads();
-        if (lane == 0) list[warp] = high;
-        __syncthreads();
-        last = list[0];
-#pragma unroll
-        for (int q = 1; q < NW; ++q) last = list[q] > last ? list[q] : last;
-        if (threadIdx.x == 0) best[k] = last;
+        if (threadIdx.x == 0) write_row(a, row, r, t);
+        const float ls = log_sum(t);
+        by_rank<NT>(list, total, a.top, [&](int k, unsigned long long key) { answer(k, key, t, ls); });
       }
     }
   }
-  if (cluster == 1) {
-    __syncthreads();
-    const Stats t = part;
-    if (threadIdx.x == 0) write_row(a, row, r, t);
-    const float ls = log_sum(t);
-    for (int k = threadIdx.x; k < a.top; k += NT) {
-      const int v = key_token(best[k]);
-      a.top_id[(i64)r * a.top + k] = v;
-      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(row[v]), t, ls);
-    }
-    return;
-  }
-  // the first block joins what the others have found
-  cg::cluster_group all = cg::this_cluster();
-  all.sync();
-  if (rank == 0) {
-    Stats t = part;
-    for (int c = 1; c < cluster; ++c) t = joined(t, *all.map_shared_rank(&part, c));
-    int total = 0;
-    for (int c = 0; c < cluster; ++c) {        // (the same arithmetic as above tells how many each has)
-      const int clo = c * share, cn = max(0, min(at.vecs - clo, share));
-      const int cf = max(0, clo * E - at.skip), ce = min(a.V, (clo + cn) * E - at.skip), ch = min(a.top, max(0, ce - cf));
-      const unsigned long long* from = all.map_shared_rank(best, c);
-      for (int k = threadIdx.x; k < ch; k += NT) list[total + k] = from[k];
-      total += ch;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) write_row(a, row, r, t);
-    const float ls = log_sum(t);
-    by_rank<NT>(list, total, a.top, [&](int k, unsigned long long key) {
-      const int v = key_token(key);
-      a.top_id[(i64)r * a.top + k] = v;
-      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(row[v]), t, ls);
-    });
-  }
-  all.sync();                                  // nobody leaves while its shared memory may be read
+  if (cluster > 1) cg::this_cluster().sync();  // nobody leaves while its shared memory may be read
 }
 
 // ---- log probabilities of short rows -----------------------------------------------------------------------------------------------
@@ -373,10 +462,8 @@ __global__ void __launch_bounds__(kShortThreads) logprob_short_kernel(const T* _
     }
     last = high;
     if (l == 0 && live) {
-      const int v = key_token(last);
-      const unsigned u = (unsigned)(last >> 32) ^ 0x80000000u;
-      a.top_id[(i64)r * a.top + k] = v;
-      a.top_logprob[(i64)r * a.top + k] = logprob_of((last >> 32) == 0u ? __int_as_float(0x7fc00000) : __uint_as_float((int)u < 0 ? u ^ 0x7fffffffu : u), t, ls);
+      a.top_id[(i64)r * a.top + k] = key_token(last);
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value((unsigned)(last >> 32)), t, ls);
     }
   }
 }
@@ -493,11 +580,20 @@ __global__ void __launch_bounds__(kGradThreads) logprob_back_kernel(const T* log
     if (i < at.vecs) {
       V16<T> y;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float logp = x[q].get(e) - lse, p = ex2(logp * kLog2e);
-        float g = p == 0.f ? 0.f : -p * fmaf(ge, logp, c0);
-        if (i * E + e - at.skip == tok) g += gl;
-        y.set(e, dead ? 0.f : g);
+      for (int e = 0; e < E / 2; ++e) {
+        const F<2> logp = x[q].pair(e) + F<2>::all(-lse);
+        const F<2> p = each(logp * F<2>::all(kLog2e), [](float v, int) { return ex2(v); });
+        F<2> g = fma_(logp, F<2>::all(-ge), F<2>::all(-c0)) * p;
+        y.set_pair(e, each(g, [&](float v, int k) { return p.x[k] == 0.f ? 0.f : v; }));
+      }
+      if (dead) y.w = make_uint4(0u, 0u, 0u, 0u);
+      if (has && !dead && tok + at.skip >= i * E && tok + at.skip < i * E + E) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (i * E + e - at.skip == tok) {
+            const float logp = x[q].get(e) - lse, p = ex2(logp * kLog2e);
+            y.set(e, (p == 0.f ? 0.f : -p * fmaf(ge, logp, c0)) + gl);
+          }
       }
       if (i > 0 && i + 1 < at.vecs && to.skip == at.skip) {
         *(reinterpret_cast<uint4*>(to.base) + i) = y.w;
@@ -524,153 +620,209 @@ struct Student { float m, s; };
 // A block, or a cluster, has a row in its registers (see above).  The gradient of the whole row is scale q; the places of the teacher's
 // alternatives are written once more, by the first of those that name the same token, after the block has written the rest.
 template <class T, int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
+__global__ void __launch_bounds__(NT, 512 / NT) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
   constexpr int E = V16<T>::E, NW = NT / 32;
-  __shared__ float prob[kMaxTeacher];          // teacher: logit / tau, then probability
-  __shared__ float gap[kMaxTeacher];           // student's logit
-  __shared__ int id[kMaxTeacher];
-  __shared__ float ra[NW], rb[NW], rc[NW];
-  __shared__ Student part;
-  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  extern __shared__ uint4 staged[];
+  __shared__ float prob[2][kMaxTeacher];       // teacher: logit / tau, then probability (rows in turn: a slow warp may still read the last one's)
+  __shared__ float gap[2][kMaxTeacher];        // student's logit
+  __shared__ int id[2][kMaxTeacher];
+  __shared__ float wm[NW], wy[NW], wany[NW], wsum[NW], wmass[NW], wloss[NW];
+  __shared__ Student part[2];
+  const int rank = blockIdx.x % cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.x / cluster;
   pdl_wait();
   pdl_trigger();
-  const T* row = logits + (i64)r * a.ld;
-  T* out = dlogits + (i64)r * a.dld;
-  const RowAt<const T> at(row, a.V);
-  const RowAt<T> to(out, a.V);
-  const int share = (at.vecs + cluster - 1) / cluster, lo = rank * share, n = max(0, min(at.vecs - lo, share));
-  V16<T> x[kVecs];
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q) {
-    const int i = q * NT + threadIdx.x;
-    if (i < n) x[q] = load_vec<T>(row, at, lo + i, a.V);
-  }
-  const float inv = 1.0f / a.tau, c = kLog2e * inv;
-  const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
-  // the teacher's alternatives, while the row is on its way
-  float ym = -INFINITY, any = 0.f;
-  for (int k = threadIdx.x; k < a.K; k += NT) {
-    const int v = a.top_id[(i64)r * a.K + k];
-    const bool in = v >= 0 && v < a.V;
-    const float y = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
-    id[k] = in ? v : -1;
-    prob[k] = y;
-    gap[k] = in ? to_f32(row[v]) : -INFINITY;
-    ym = fmaxf(ym, y);                         // (a NaN shows in the sum)
-    if (y != -INFINITY) any = 1.f;
-  }
-  float m = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q)
-    if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
-  m = warp_max(m);
-  ym = warp_max(ym);
-  any = __any_sync(0xffffffffu, any != 0.f) ? 1.f : 0.f;
-  if (lane == 0) { ra[warp] = m; rb[warp] = ym; rc[warp] = any; }
-  __syncthreads();
-  m = ra[0];
-  ym = rb[0];
-  any = rc[0];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) { m = max_nan(m, ra[w]); ym = fmaxf(ym, rb[w]); any += rc[w]; }
-  __syncthreads();
-  const float m0 = ref_of(m), y0 = ref_of(ym);
-  float s = 0.f, mass = 0.f;
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q) {
-    if (q * NT + threadIdx.x < n) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += ex2((x[q].get(e) - m0) * c);
+  const Stage<T, NT> stage{logits, logits + ((i64)(a.N - 1) * a.ld + a.V), a.ld, a.V, cluster, rank, staged + threadIdx.x};
+  const float inv = 1.0f / a.tau, c = kLog2e * inv, uniform = 1.0f / (float)a.N;
+  int r = blockIdx.x / cluster;
+  if (r < a.N) stage.bring(r);
+  copies_issued();
+  // The thread's first alternative is fetched ahead: its token and logit two rows, the student's logit of that token one row.
+  struct Teacher { int v; float y, z; };
+  const bool teaches = warp * 32 < a.K;        // (the other warps have no alternatives)
+  const auto named = [&](int row, int k) {
+    Teacher t{-1, -INFINITY, -INFINITY};
+    if (row < a.N && k < a.K) {
+      t.v = a.top_id[(i64)row * a.K + k];
+      t.y = a.top_logit[(i64)row * a.K + k];
     }
+    return t;
+  };
+  const auto look_up = [&](Teacher& t, int row) {
+    if (t.v >= 0 && t.v < a.V) t.z = to_f32(logits[(i64)row * a.ld + t.v]);
+    else t.v = -1;
+  };
+  const auto weight_of = [&](int row) { return a.weight ? a.weight[min(row, a.N - 1)] : uniform; };
+  Teacher now{-1, -INFINITY, -INFINITY}, soon = now;
+  if (teaches) {
+    now = named(r, threadIdx.x);
+    look_up(now, r);
+    soon = named(r + step, threadIdx.x);
   }
-  for (int k = threadIdx.x; k < a.K; k += NT) mass += ex2((prob[k] - y0) * kLog2e);
-  s = warp_sum(s);
-  mass = warp_sum(mass);
-  if (lane == 0) { ra[warp] = s; rb[warp] = mass; }
-  __syncthreads();
-  s = mass = 0.f;
+  float next_weight = weight_of(r);
+  // Elements of vectors that the row only has a part of, written one by one by the last warp: lanes 0.. those of its first vector, lanes
+  // 16.. those of its last one; the logits are fetched a row ahead.
+  const auto edge_of = [&](int row) {
+    if (warp != NW - 1 || row >= a.N || (lane & 15) >= E) return -1;
+    const RowAt<const T> at(logits + (i64)row * a.ld, a.V);
+    const int per = stage.share(at), e = lane & 15, v = (lane < 16 ? 0 : (at.vecs - 1) * E) + e - at.skip;
+    if (v < 0 || v >= a.V) return -1;
+    const bool partial = lane < 16 ? at.skip > 0 : at.vecs * E > a.V + at.skip;
+    const int owner = (lane < 16 ? 0 : at.vecs - 1) / per;
+    return partial && owner == rank ? v : -1;
+  };
+  int edge = edge_of(r);
+  float edge_logit = edge >= 0 ? to_f32(logits[(i64)r * a.ld + edge]) : 0.f;
+  for (int buf = 0; r < a.N; r += step, buf ^= 1) {
+    const T* row = logits + (i64)r * a.ld;
+    T* out = dlogits + (i64)r * a.dld;
+    const float weight = next_weight;
+    next_weight = weight_of(r + step);
+    float ym = -INFINITY;
+    bool any = false;
+    if (teaches) {
+      for (int k = threadIdx.x; k < a.K; k += NT) {
+        Teacher t = now;
+        if (k >= NT) {
+          t = named(r, k);
+          look_up(t, r);
+        }
+        const float y = t.v >= 0 ? t.y * inv : -INFINITY;
+        id[buf][k] = t.v;
+        prob[buf][k] = y;
+        gap[buf][k] = t.v >= 0 ? t.z : -INFINITY;
+        ym = fmaxf(ym, y);                     // (a NaN shows in the sum)
+        any = any || y != -INFINITY;
+      }
+      now = soon;
+      look_up(now, r + step);
+      soon = named(r + 2 * step, threadIdx.x);
+      ym = warp_max(ym);
+      any = __any_sync(0xffffffffu, any);
+    }
+    V16<T> x[kVecs];
+    int lo;
+    const int n = stage.take(r, x, lo);
+    if (r + step < a.N) stage.bring(r + step);
+    copies_issued();
+    const RowAt<const T> at(row, a.V);
+    const RowAt<T> to(out, a.V);
+    float m = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { s += ra[w]; mass += rb[w]; }
-  float M = m0;
-  if (cluster > 1) {
-    cg::cluster_group all = cg::this_cluster();
-    if (threadIdx.x == 0) part = Student{m, s};
-    all.sync();                                // (also: every block has read what it needs before the first gradient is written)
-    Student each[kMaxCluster];
-    M = -INFINITY;
+    for (int q = 0; q < kVecs; ++q)
+      if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
+    m = warp_max(m);
+    if (lane == 0) { wm[warp] = m; wy[warp] = ym; wany[warp] = any ? 1.f : 0.f; }
+    __syncthreads();
+    m = all_max<NW>(wm);
+    ym = all_max<NW>(wy);
+    const float present = all_max<NW>(wany);
+    const float m0 = ref_of(m), y0 = ref_of(ym);
+    const F<2> scale = F<2>::all(c);
+    F<2> sum = F<2>::all(0.f);
+    float mass = 0.f;
 #pragma unroll
-    for (int q = 0; q < kMaxCluster; ++q) {
-      if (q < cluster) {
-        each[q] = *all.map_shared_rank(&part, q);
-        M = max_nan(M, each[q].m);
+    for (int q = 0; q < kVecs; ++q) {
+      if (q * NT + threadIdx.x < n) {
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) sum = sum + each((x[q].pair(e) + F<2>::all(-m0)) * scale, [](float v, int) { return ex2(v); });
       }
     }
-    all.barrier_arrive();                      // (waited for at the end: nobody leaves while its shared memory may be read)
-    M = ref_of(M);
-    s = 0.f;
-#pragma unroll
-    for (int q = 0; q < kMaxCluster; ++q)
-      if (q < cluster) s += each[q].s == 0.f ? 0.f : each[q].s * ex2((each[q].m - M) * c);
-  }
-  const float ls = logf(s), lmass = logf(mass), scale = weight * a.tau;
-  float loss = 0.f;
-  for (int k = threadIdx.x; k < a.K; k += NT) {
-    const float logp = (prob[k] - y0) - lmass, p = ex2(logp * kLog2e), z = gap[k];
-    const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
-    loss += p == 0.f ? 0.f : p * (logp - logq);
-    prob[k] = p;
-  }
-  if (rank == 0) {
-    loss = warp_sum(loss);
-    if (lane == 0) rc[warp] = loss;
-  }
-  const bool none = any == 0.f || weight == 0.f;
-  const float f = none || s == 0.f ? 0.f : scale / s;
-#pragma unroll
-  for (int q = 0; q < kVecs; ++q) {
-    const int j = q * NT + threadIdx.x, i = lo + j;
-    if (j < n) {
-      V16<T> y;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float g = ex2((x[q].get(e) - M) * c) * f;
-        y.set(e, none ? 0.f : g);
+    if (teaches) {
+      for (int k = threadIdx.x; k < a.K; k += NT) mass += ex2((prob[buf][k] - y0) * kLog2e);
+      mass = warp_sum(mass);
+    }
+    float s = warp_sum(sum.x[0] + sum.x[1]);
+    if (lane == 0) { wsum[warp] = s; wmass[warp] = mass; }
+    __syncthreads();
+    s = all_sum<NW>(wsum);
+    float M = m0;
+    if (cluster > 1) {
+      cg::cluster_group all = cg::this_cluster();
+      if (threadIdx.x == 0) part[buf] = Student{m, s};
+      all.sync();                              // (also: every block has read what it needs before the first gradient is written)
+      const Student b = lane < cluster ? *all.map_shared_rank(&part[buf], lane) : Student{-INFINITY, 0.f};      // (one trip for all)
+      M = ref_of(warp_max(b.m));
+      s = warp_sum(b.s == 0.f ? 0.f : b.s * ex2((b.m - M) * c));
+    }
+    const float gain = weight * a.tau;
+    float loss = 0.f;
+    if (teaches) {
+      const float ls = logf(s), lmass = logf(all_sum<NW>(wmass));
+      for (int k = threadIdx.x; k < a.K; k += NT) {
+        const float logp = (prob[buf][k] - y0) - lmass, p = ex2(logp * kLog2e), z = gap[buf][k];
+        const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
+        loss += p == 0.f ? 0.f : p * (logp - logq);
+        prob[buf][k] = p;
       }
-      if (i > 0 && i + 1 < at.vecs && to.skip == at.skip) {
-        __stcs(reinterpret_cast<uint4*>(to.base) + i, y.w);
+      loss = warp_sum(loss);
+    }
+    if (lane == 0) wloss[warp] = loss;
+    const bool none = present == 0.f || weight == 0.f;
+    const F<2> f = F<2>::all(s == 0.f ? 0.f : gain / s), from = F<2>::all(-M);
+    const int whole_from = lo == 0 && at.skip > 0 ? 1 : 0;      // vectors that are the row's alone
+    const int left = n - (lo + n == at.vecs && at.vecs * E > a.V + at.skip ? 1 : 0) - (int)threadIdx.x;
+    if (to.skip == at.skip) {
+      uint4* dst = reinterpret_cast<uint4*>(to.base) + lo + threadIdx.x;
+      if (!none) {
+#pragma unroll
+        for (int q = 0; q < kVecs; ++q) {
+          if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) {
+            V16<T> y;
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) y.set_pair(e, each((x[q].pair(e) + from) * scale, [](float v, int) { return ex2(v); }) * f);
+            __stcs(dst + q * NT, y.w);
+          }
+        }
       } else {
+#pragma unroll 1
+        for (int q = 0; q < kVecs; ++q)
+          if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) __stcs(dst + q * NT, make_uint4(0u, 0u, 0u, 0u));
+      }
+    } else {                                   // rows of the two arrays start at different places of a vector
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int v = i * E + e - at.skip;
-          if (v >= 0 && v < a.V) out[v] = y.raw(e);
+      for (int q = 0; q < kVecs; ++q) {
+        if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) {
+          T* dst = out + (i64)(lo + q * NT + (int)threadIdx.x) * E - at.skip;
+#pragma unroll
+          for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(none ? 0.f : ex2((x[q].get(e) - M) * c) * f.x[0]);
+        }
+      }
+    }
+    if (warp == NW - 1) {
+      if (edge >= 0) out[edge] = from_f32<T>(none ? 0.f : ex2((edge_logit - M) * c) * f.x[0]);
+      edge = edge_of(r + step);
+      edge_logit = edge >= 0 ? to_f32(logits[(i64)(r + step) * a.ld + edge]) : 0.f;
+    }
+    __syncthreads();
+    if (rank == 0 && warp == NW - 1) {
+      const float t = all_sum<NW>(wloss);
+      if (lane == 0) a.row_loss[r] = present != 0.f ? a.tau * a.tau * t : 0.f;
+    }
+    if (!none && teaches) {
+      const int begin = lo * E - at.skip, stop = (lo + n) * E - at.skip;      // the block's own tokens
+      for (int k0 = warp * 32; k0 < a.K; k0 += NT) {
+        const int k = k0 + lane, v = k < a.K ? id[buf][k] : -1;
+        float p = k < a.K ? prob[buf][k] : 0.f;
+        bool first = true;
+        const int namesakes = __popc(__match_any_sync(0xffffffffu, v));      // (every lane takes part)
+        if (a.K > 32 || __any_sync(0xffffffffu, v >= 0 && namesakes > 1)) {
+          // the same token may be named twice: its first place adds all of them up, in their order
+          p = 0.f;
+#pragma unroll 4
+          for (int j = 0; j < a.K; ++j) {
+            const bool same = id[buf][j] == v;
+            first = first && !(same && j < k);
+            p += same ? prob[buf][j] : 0.f;
+          }
+        }
+        if (v >= 0 && v >= begin && v < stop && first) {
+          const float q = s == 0.f ? 0.f : ex2((gap[buf][k] - M) * c) / s;
+          out[v] = from_f32<T>(gain * (q - p));
         }
       }
     }
   }
-  __syncthreads();
-  if (rank == 0 && threadIdx.x == 0) {
-    float t = 0.f;
-    for (int w = 0; w < NW; ++w) t += rc[w];
-    a.row_loss[r] = any != 0.f ? a.tau * a.tau * t : 0.f;
-  }
-  if (!none) {
-    const int first = lo * E - at.skip, end = (lo + n) * E - at.skip;      // the block's own tokens
-    for (int k = threadIdx.x; k < a.K; k += NT) {
-      const int v = id[k];
-      if (v < 0 || v < first || v >= end) continue;
-      float p = 0.f;
-      bool again = false;
-      for (int j = 0; j < a.K; ++j) {
-        if (id[j] != v) continue;
-        again = again || j < k;
-        p += prob[j];
-      }
-      if (again) continue;
-      const float q = s == 0.f ? 0.f : ex2((gap[k] - M) * c) / s;
-      out[v] = from_f32<T>(scale * (q - p));
-    }
-  }
-  if (cluster > 1) cg::this_cluster().barrier_wait();
+  if (cluster > 1) cg::this_cluster().sync();  // nobody leaves while its shared memory may be read
 }
 
 // Short rows: G lanes have a row, PER logits each; the teacher's probabilities of each token meet in shared memory, in the order of the
@@ -860,25 +1012,33 @@ int launched(cudaError_t e) {
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
-// Blocks that share a row of `vecs` vectors, and their threads.  The fewest that hold it, 128 threads where they suffice; where that leaves
+// Blocks that share a row of `vecs` vectors, and their threads.  The fewest that hold it, 64 threads where they suffice; where that leaves
 // SMs without work, more of them, down to two vectors a thread (8 rows of 131072 in bf16: 21 us on 32 blocks, 9 on 128).  0: too long.
 struct Split { int cluster, threads; };
 Split split_of(int N, i64 vecs) {
-  const i64 whole = 512 * kVecs;
-  if (vecs > kMaxCluster * whole) return {0, 0};
-  if (vecs <= 128 * kVecs && (i64)N * ((vecs + 255) / 256) >= 296) return {1, 128};
+  if (vecs > (i64)kMaxCluster * 512 * kVecs) return {0, 0};
+  if (vecs <= 64 * kVecs && (i64)N * ((vecs + 255) / 256) >= 296) return {1, 64};
   int c = 1;
-  while ((vecs + c - 1) / c > whole) c *= 2;
+  const int threads = vecs <= 256 * kVecs ? 256 : 512;
+  while ((vecs + c - 1) / c > threads * kVecs) c *= 2;
   while (c < kMaxCluster && (i64)N * c < 148 && vecs / (2 * c) >= 1024) c *= 2;
-  return {c, 512};
+  return {c, (vecs + c - 1) / c <= 256 * kVecs ? 256 : 512};
 }
-template <class... KArgs, class... Args>
-cudaError_t launch_rows(void (*kern)(KArgs...), int N, Split sp, cudaStream_t s, Args&&... args) {
-  if (sp.cluster > 8) {                        // more than the portable size
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
+// Blocks stay for several rows, each with the next one on its way.
+template <class K, class T, class... Args> cudaError_t launch_rows(K kern, int N, Split sp, cudaStream_t s, int (&known)[kMaxDevices], const T* x, Args&&... args) {
+  const int dev = current_device_slot(), smem = kVecs * sp.threads * 16;
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (!known[dev]) {
+    int per_sm = 0, sms = 0;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, sp.threads, smem);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess || per_sm * sms == 0) return e != cudaSuccess ? e : cudaErrorInvalidConfiguration;
+    known[dev] = per_sm * sms;
   }
-  return launch_pdl_cluster(kern, sp.cluster, dim3((unsigned)N * sp.cluster), dim3(sp.threads), 0, s, static_cast<Args&&>(args)..., sp.cluster);
+  const int most = known[dev] / sp.cluster, groups = N < most ? N : most;
+  return launch_pdl_cluster(kern, sp.cluster, dim3((unsigned)(groups * sp.cluster)), dim3(sp.threads), (size_t)smem, s, x, static_cast<Args&&>(args)..., sp.cluster);
 }
 // vectors of a row; one more where rows start inside a vector
 i64 vecs_of(int V, int dtype, const void* p, i64 ld) {
@@ -907,13 +1067,15 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
     const T* x = static_cast<const T*>(logits);
     cudaStream_t s = (cudaStream_t)stream;
     const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
+    static int known[3][kMaxDevices];          // resident blocks of the three kernels, by device
     const auto few = [&](auto kern, int lanes) { e = launch_pdl(kern, dim3((unsigned)(((i64)N * lanes + kShortThreads - 1) / kShortThreads)), dim3(kShortThreads), 0, s, x, a); };
     if (V <= 64) few(logprob_short_kernel<T, 8, 8>, 8);
     else if (V <= 256) few(logprob_short_kernel<T, 32, 8>, 32);
     else if (V <= kShortRow) few(logprob_short_kernel<T, 32, 32>, 32);
     else if (sp.cluster == 0) e = launch_pdl(logprob_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, a);
-    else if (sp.threads == 128) e = launch_rows(logprob_kernel<T, 128>, N, sp, s, x, a);
-    else e = launch_rows(logprob_kernel<T, 512>, N, sp, s, x, a);
+    else if (sp.threads == 64) e = launch_rows(logprob_kernel<T, 64>, N, sp, s, known[0], x, a);
+    else if (sp.threads == 256) e = launch_rows(logprob_kernel<T, 256>, N, sp, s, known[1], x, a);
+    else e = launch_rows(logprob_kernel<T, 512>, N, sp, s, known[2], x, a);
   });
   return launched(e);
 }
@@ -962,6 +1124,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
       const T* x = static_cast<const T*>(logits);
       T* d = static_cast<T*>(dlogits);
       const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
+      static int known[3][kMaxDevices];        // resident blocks of the three kernels, by device
       const auto few = [&](auto kern, int lanes) {
         const i64 blocks = ((i64)N * lanes + kShortThreads - 1) / kShortThreads;
         added = blocks == 1;
@@ -971,8 +1134,9 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
       else if (V <= 256) few(distill_short_kernel<T, 32, 8>, 32);
       else if (V <= kShortRow) few(distill_short_kernel<T, 32, 32>, 32);
       else if (sp.cluster == 0) e = launch_pdl(distill_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, d, a);
-      else if (sp.threads == 128) e = launch_rows(distill_kernel<T, 128>, N, sp, s, x, d, a);
-      else e = launch_rows(distill_kernel<T, 512>, N, sp, s, x, d, a);
+      else if (sp.threads == 64) e = launch_rows(distill_kernel<T, 64>, N, sp, s, known[0], x, d, a);
+    else if (sp.threads == 256) e = launch_rows(distill_kernel<T, 256>, N, sp, s, known[1], x, d, a);
+      else e = launch_rows(distill_kernel<T, 512>, N, sp, s, known[2], x, d, a);
     });
     rc = launched(e);
     if (rc != MGRIT_OK || added) return rc;

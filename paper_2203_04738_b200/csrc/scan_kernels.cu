@@ -79,60 +79,9 @@ constexpr int kPairs = 2;                      // pairs of a column in flight in
 constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
 constexpr float kMaxDt = 1e18f;
 
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp_exact(float x) { const float y = rcp(x); return fmaf(fmaf(-x, y, 1.0f), y, y); }      // one Newton step
 
-#ifndef SCAN_SCALAR
-#define SCAN_SCALAR 0
-#endif
-// VC columns side by side.  Two of them use the packed fp32 instructions, which take one issue slot for both: the scan of 16-bit types
-// is bound by instructions (55 an element of 6 bytes before this and the wider loads, 170 us where the bytes take 61).
-template <int VC> struct F {
-  float x[VC];
-  __device__ __forceinline__ static F all(float v) {
-    F f;
-#pragma unroll
-    for (int i = 0; i < VC; ++i) f.x[i] = v;
-    return f;
-  }
-  __device__ __forceinline__ float& at(int i) { return x[i]; }
-  __device__ __forceinline__ float at(int i) const { return x[i]; }
-};
-template <int VC> __device__ __forceinline__ F<VC> operator*(const F<VC>& a, const F<VC>& b) {
-  F<VC> r;
-  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = a.x[i] * b.x[i]; return r; }
-#pragma unroll
-  for (int i = 0; i + 1 < VC; i += 2)
-    asm("{.reg .b64 p, q, r; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; mul.rn.f32x2 r, p, q; mov.b64 {%0, %1}, r;}"
-        : "=f"(r.x[i]), "=f"(r.x[i + 1]) : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]));
-  return r;
-}
-template <int VC> __device__ __forceinline__ F<VC> operator+(const F<VC>& a, const F<VC>& b) {
-  F<VC> r;
-  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = a.x[i] + b.x[i]; return r; }
-#pragma unroll
-  for (int i = 0; i + 1 < VC; i += 2)
-    asm("{.reg .b64 p, q, r; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; add.rn.f32x2 r, p, q; mov.b64 {%0, %1}, r;}"
-        : "=f"(r.x[i]), "=f"(r.x[i + 1]) : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]));
-  return r;
-}
-template <int VC> __device__ __forceinline__ F<VC> fma_(const F<VC>& a, const F<VC>& b, const F<VC>& c) {
-  F<VC> r;
-  if (VC == 1 || SCAN_SCALAR) { for (int i = 0; i < VC; ++i) r.x[i] = fmaf(a.x[i], b.x[i], c.x[i]); return r; }
-#pragma unroll
-  for (int i = 0; i + 1 < VC; i += 2)
-    asm("{.reg .b64 p, q, r, s; mov.b64 p, {%2, %3}; mov.b64 q, {%4, %5}; mov.b64 r, {%6, %7}; fma.rn.f32x2 s, p, q, r; mov.b64 {%0, %1}, s;}"
-        : "=f"(r.x[i]), "=f"(r.x[i + 1])
-        : "f"(a.x[i]), "f"(a.x[i + 1]), "f"(b.x[i]), "f"(b.x[i + 1]), "f"(c.x[i]), "f"(c.x[i + 1]));
-  return r;
-}
-template <int VC, class Fn> __device__ __forceinline__ F<VC> each(F<VC> a, Fn&& fn) {
-  F<VC> r;
-#pragma unroll
-  for (int i = 0; i < VC; ++i) r.at(i) = fn(a.at(i), i);
-  return r;
-}
 
 // VC consecutive elements of a row, moved as one word
 template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
