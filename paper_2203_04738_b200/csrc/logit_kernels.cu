@@ -2,14 +2,15 @@
 // distillation from a teacher's top logits.
 //
 // All are bound by HBM (a row is read once, gradients are written once) with one or two exponentials an element, which take up to three
-// quarters of that time (16 a cycle and SM).  Rows of up to 16 x kThreads x kVecs vectors are held in registers:
-//  * short rows (V <= 1024): a group of 8 or 32 lanes has a row;
-//  * longer ones: a block, or a cluster of up to 16 blocks that share a row and meet through distributed shared memory.  A thread
-//    loads all of its 16-byte vectors at once, the next row's while it works on one, so that the largest logit, the sums, the top alternatives and the gradient are all
-//    formed without reading a row again, and without the rescaling that running sums need.  Few rows are split over more blocks than
-//    they need, so that a single token's row of 131072 is read by 16 SMs;
-//  * rows beyond that: a block per row in several passes (only their first one from HBM, the others mostly from L2).
-// Rows may start anywhere: vectors are aligned in memory, the first and the last one of a row are read element by element.
+// quarters of that time (16 a cycle and SM).
+//  * short rows (V <= 1024): a group of 8 or 32 lanes has a row, in registers;
+//  * longer ones: a block, or a cluster of up to 16 that meet through distributed shared memory, one for about 64 KB of a row.  The first
+//    pass streams the row once with a reference for the exponents that only moves when it has to; what is looked at twice (the gradient's
+//    pass, the vectors that hold a top alternative) comes from L2, where the rows in work have room.  Small blocks and no state but the
+//    sums: holding a row in registers or shared memory instead took 138 us for distillation of 4096 x 32768 in bf16 (bytes: 82), bound
+//    by the length and the latency of its code with 16 warps on an SM.  Few rows are split further, so that one token's row of 131072 is
+//    read by 16 SMs.
+// Rows may start anywhere: whole 16-byte vectors that are the row's alone are moved as such, the few elements around them one by one.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -21,7 +22,7 @@ namespace mg {
 namespace {
 
 constexpr int kMaxTop = 128, kMaxTeacher = 1024;
-constexpr int kVecs = 16;                      // 16-byte vectors of a thread
+constexpr int kRow = 256, kBatch = 4;          // threads of a block, 16-byte vectors of a thread at a time
 constexpr int kMaxCluster = 16;
 constexpr int kShortRow = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -80,89 +81,62 @@ template <class T> __device__ __forceinline__ float max_of(const V16<T>& v) {
   }
 }
 
-// A row's place in memory: `skip` elements lie between the 16-byte word in which it starts and its first element
-template <class T> struct RowAt {
-  T* base;                                     // that word
-  int skip, vecs;                              // vectors that hold some of the row
-  __device__ __forceinline__ RowAt(T* row, int V) {
-    skip = (int)(((uintptr_t)row & 15u) / sizeof(T));
-    base = row - skip;
-    vecs = (int)(((i64)V + skip + V16<T>::E - 1) / V16<T>::E);
+// A block's part of a row: n whole vectors from `first`, element v0 of the row on; and at most one of the row's other elements for each
+// lane of the first warp (in front of the row's first whole vector, behind its last one)
+template <class T> struct Part {
+  static constexpr int E = V16<T>::E;
+  i64 n; int v0, edge;
+  const uint4* first;
+  __device__ __forceinline__ Part(const T* row, int V, int cluster, int rank) {
+    const int skip = (int)((16u - ((uintptr_t)row & 15u)) & 15u) / (int)sizeof(T), head = min(skip, V), vecs = (V - head) / E;
+    const int per = (vecs + cluster - 1) / cluster, lo = min(vecs, rank * per);
+    n = min(vecs - lo, per);
+    v0 = head + lo * E;
+    first = reinterpret_cast<const uint4*>(row + v0);
+    const int l = (int)threadIdx.x, tail = V - head - vecs * E;
+    edge = -1;
+    if (l < 8 && rank == 0 && l < head) edge = l;
+    if (l >= 8 && l < 16 && rank == cluster - 1 && l - 8 < tail) edge = head + vecs * E + l - 8;
   }
 };
-template <class T> __device__ __forceinline__ V16<T> load_vec(const T* row, const RowAt<const T>& at, int i, int V) {
+// how many elements block `rank` of the cluster has
+template <class T> __device__ __forceinline__ int elements_of(const T* row, int V, int cluster, int rank) {
   constexpr int E = V16<T>::E;
-  V16<T> v;
-  if (i > 0 && i + 1 < at.vecs) {
-    v.w = __ldcs(reinterpret_cast<const uint4*>(at.base) + i);
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int k = i * E + e - at.skip;
-      v.raw(e) = k >= 0 && k < V ? row[k] : from_f32<T>(-INFINITY);
-    }
-  }
-  return v;
+  const int skip = (int)((16u - ((uintptr_t)row & 15u)) & 15u) / (int)sizeof(T), head = min(skip, V), vecs = (V - head) / E;
+  const int per = (vecs + cluster - 1) / cluster, lo = min(vecs, rank * per);
+  return min(vecs - lo, per) * E + (rank == 0 ? head : 0) + (rank == cluster - 1 ? V - head - vecs * E : 0);
 }
 
-// A block's share of a row on its way to registers: a thread copies its vectors to its own places in shared memory, asynchronously, while the
-// row before is worked on, and reads them back itself, so nobody waits for anybody.  Vectors at a row's ends are copied whole where the
-// bytes around the row belong to the array (they are replaced by -inf when read back), and element by element where they do not.
-template <class T, int NT> struct Stage {
-  static constexpr int E = V16<T>::E;
-  const T *first, *end;                        // the array
-  i64 ld;
-  int V, cluster, rank;
-  uint4* mine;                                 // the thread's places, NT apart
-  __device__ __forceinline__ int share(const RowAt<const T>& at) const { return (at.vecs + cluster - 1) / cluster; }
-  __device__ __forceinline__ void bring(i64 r) const {
-    const T* row = first + r * ld;
-    const RowAt<const T> at(row, V);
-    const int per = share(at), lo = rank * per, n = max(0, min(at.vecs - lo, per));
-    const T* p = at.base + (i64)(lo + (int)threadIdx.x) * E;
-    const unsigned to = (unsigned)__cvta_generic_to_shared(mine);
-    // all but the array's own ends, where a vector would reach outside
-    const bool cut_head = lo == 0 && at.base < first, cut_tail = n > 0 && at.base + (i64)(lo + n) * E > end;
-    const int left = n - (cut_tail ? 1 : 0) - (int)threadIdx.x;
+// What a thread has seen of a row: the largest logit, m; s = sum 2^((x - r) c) and w, the same terms times their exponents, for a reference r that
+// follows the largest logit only when that has left it far behind (the terms stay below 2^44, the sums in range).
+struct Seen {
+  float m = -INFINITY, r = -3.4028235e38f;
+  F<2> s = F<2>::all(0.f), w = F<2>::all(0.f);
+  __device__ __forceinline__ void follow(float top, float c) {
+    m = max_nan(m, top);
+    if ((top - r) * c > 40.f) {                // (the first time: r is the lowest value there is)
+      const float d = (r - top) * c, f = ex2(d);
 #pragma unroll
-    for (int q = 0; q < kVecs; ++q)
-      if (q * NT < left && !(q == 0 && cut_head && threadIdx.x == 0))
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + q * (NT * 16)), "l"(p + q * (NT * E)) : "memory");
-    if (cut_head || cut_tail) {
-#pragma unroll 1
-      for (int q = 0; q < kVecs; ++q) {
-        const int i = q * NT + (int)threadIdx.x;
-        if ((cut_head && i == 0) || (cut_tail && i == n - 1)) {
-#pragma unroll 1
-          for (int e = 0; e < E; ++e) {
-            const T* from = p + (i64)q * (NT * E) + e;
-            if (from >= first && from < end) reinterpret_cast<T*>(mine + q * NT)[e] = *from;
-          }
-        }
+      for (int i = 0; i < 2; ++i) {
+        w.x[i] = f == 0.f ? 0.f : f * fmaf(s.x[i], d, w.x[i]);
+        s.x[i] *= f;
       }
+      r = top;
     }
   }
-  // -> the number of the block's vectors, and where they start in the row
-  __device__ __forceinline__ int take(i64 r, V16<T> (&x)[kVecs], int& lo) const {
-    const RowAt<const T> at(first + r * ld, V);
-    const int per = share(at);
-    lo = rank * per;
-    const int n = max(0, min(at.vecs - lo, per));
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    if (lo == 0 && threadIdx.x == 0)
-#pragma unroll 1
-      for (int e = 0; e < at.skip; ++e) reinterpret_cast<T*>(mine)[e] = from_f32<T>(-INFINITY);
-    const int last = at.vecs - 1 - lo;         // the row's last vector, counted from the block's first
-    if (last >= 0 && last < n && last % NT == (int)threadIdx.x)
-#pragma unroll 1
-      for (int e = V + at.skip - (at.vecs - 1) * E; e < E; ++e) reinterpret_cast<T*>(mine + last / NT * NT)[e] = from_f32<T>(-INFINITY);
-#pragma unroll
-    for (int q = 0; q < kVecs; ++q)
-      if (q * NT < n - (int)threadIdx.x) x[q].w = mine[q * NT];
-    return n;
+  // W: with w.  Exponents stop at -150 there, where the terms are zero (a term of -inf would make 0 x inf of its product).
+  template <bool W> __device__ __forceinline__ void add(const F<2>& x, float c) {
+    F<2> t = (x + F<2>::all(-r)) * F<2>::all(c);
+    if (W) t = each(t, [](float v, int) { return fmaxf(v, -150.f); });
+    const F<2> y = each(t, [](float v, int) { return ex2(v); });
+    s = s + y;
+    if (W) w = fma_(y, t, w);
   }
 };
-__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <bool W, class T> __device__ __forceinline__ void see_edge(Seen& t, float x, float c) {
+  t.follow(x, c);
+  t.add<W>(F<2>{{x, -INFINITY}}, c);
+}
 
 // ---- reductions over a block -----------------------------------------------------------------------------------------------------
 
@@ -229,176 +203,186 @@ template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsig
   }
 }
 
-// The top alternatives: a warp's lanes have the largest logit each of their own share, and the warp's j-th largest of these, j = top /
-// warps rounded up, is a bound: at least j of its logits reach it.  So at least `top` logits reach the lowest of the warps' bounds, and
-// those that do are few (some hundred of 32768 random ones for top = 20); they are put in order by counting.  Where ties or a NaN
-// make them many, the largest is taken out `top` times instead.
-template <class T, int NT>
-__global__ void __launch_bounds__(NT, 512 / NT) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
-  constexpr int E = V16<T>::E, NW = NT / 32;
-  extern __shared__ uint4 staged[];
-  __shared__ unsigned long long list[kList];
-  __shared__ unsigned long long best[2][kMaxTop];
-  __shared__ float wmax[NW], wbound[NW], wsum[NW], wdot[NW];
-  __shared__ Stats part[2];
-  __shared__ int count[2];
-  const int rank = blockIdx.x % cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.x / cluster;
+// The top alternatives: every warp names the j largest of its threads' largest logits, j = top / warps rounded up; the top-th largest of all that
+// are named is a bound that at least `top` logits reach (top > 32: the lowest of them).  Only threads whose largest logit reaches it look at
+// their logits again, as a rule at one batch of them, since a thread knows the largest logit of its best batch and of all the others.  What
+// they find, little more than `top`, is put in order by counting.  Where ties or a NaN make it much, the largest is taken out `top` times.
+template <class T, bool TOP>
+__global__ void __launch_bounds__(kRow, 4) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
+  constexpr int E = V16<T>::E, NW = kRow / 32;
+  __shared__ unsigned long long list[TOP ? kList : 1];
+  __shared__ unsigned long long best[TOP ? kMaxTop : 1];
+  __shared__ float wmax[NW], wsum[NW], wdot[NW];
+  __shared__ unsigned named[TOP ? kMaxTop + 32 : 1];
+  __shared__ Stats part;
+  __shared__ int count;
+  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  const Stage<T, NT> stage{logits, logits + ((i64)(a.N - 1) * a.ld + a.V), a.ld, a.V, cluster, rank, staged + threadIdx.x};
-  int r = blockIdx.x / cluster;
-  if (r < a.N) stage.bring(r);
-  copies_issued();
-  if (threadIdx.x < 2) count[threadIdx.x] = 0;
-  for (int buf = 0; r < a.N; r += step, buf ^= 1) {
-    V16<T> x[kVecs];
-    int lo;
-    const int n = stage.take(r, x, lo);        // the block's vectors
-    if (r + step < a.N) stage.bring(r + step);
-    copies_issued();
-    const T* row = logits + (i64)r * a.ld;
-    const RowAt<const T> at(row, a.V);
+  const T* row = logits + (i64)r * a.ld;
+  const Part<T> p(row, a.V, cluster, rank);
+  if (threadIdx.x == 0) count = 0;
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
+  Seen t;
+  float high = -INFINITY, others = -INFINITY;  // largest logits of the thread's best batch and of the rest
+  int where = -1;
+  for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * kRow < p.n) x[q].w = __ldg(p.first + i + q * kRow);
     float m = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < kVecs; ++q)
-      if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
-    const float mine = m;
-    m = warp_max(m);
-    if (lane == 0) wmax[warp] = m;
-    if (a.top > 0) {
-      // the warp's j-th largest of its lanes' largest logits; warps without logits have no say
-      const int warps = max(1, min(NW, (n + 31) / 32)), j = (a.top + warps - 1) / warps;
-      unsigned k = value_key(mine), b = 0u;
-      for (int i = 0; i < min(j, 32); ++i) {
-        b = __reduce_max_sync(0xffffffffu, k);
-        const unsigned who = __ballot_sync(0xffffffffu, k == b);
-        if (lane == __ffs(who) - 1) k = 0u;
-      }
-      if (j > 32) b = 0u;
-      if (lane == 0) wbound[warp] = warp * 32 < n ? (b == 0u ? INFINITY : -key_value(b)) : -INFINITY;
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * kRow < p.n) m = max_nan(m, max_of(x[q]));
+    t.follow(m, kLog2e);
+    if (TOP) {
+      if (m > high) { others = high; high = m; where = i; }
+      else others = fmaxf(others, m);
     }
-    __syncthreads();
-    m = all_max<NW>(wmax);
-    // sums: exponents stop at -150, where the terms are zero (a term of -inf would make 0 x inf of its product)
-    const float m0 = ref_of(m);
-    F<2> s = F<2>::all(0.f), w = F<2>::all(0.f);
-    const F<2> from = F<2>::all(-m0), scale = F<2>::all(kLog2e);
 #pragma unroll
-    for (int q = 0; q < kVecs; ++q) {
-      if (q * NT + threadIdx.x < n) {
+    for (int q = 0; q < kBatch; ++q) {
+      if (i + q * kRow < p.n) {
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          const F<2> t = each((x[q].pair(e) + from) * scale, [](float v, int) { return fmaxf(v, -150.f); });
-          const F<2> y = each(t, [](float v, int) { return ex2(v); });
-          s = s + y;
-          w = fma_(y, t, w);
-        }
-      }
-    }
-    const float s1 = warp_sum(s.x[0] + s.x[1]), w1 = warp_sum(w.x[0] + w.x[1]);
-    if (lane == 0) { wsum[warp] = s1; wdot[warp] = w1; }
-    if (threadIdx.x == 0) count[buf ^ 1] = 0;
-    if (a.top > 0) {
-      const float bound = -all_max<NW>(wbound);      // (they are kept with their signs turned)
-      if (mine >= bound) {
-#pragma unroll
-        for (int q = 0; q < kVecs; ++q) {
-          if (q * NT + threadIdx.x < n && max_of(x[q]) >= bound) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
-              if (x[q].get(e) >= bound && v >= 0 && v < a.V) {
-                const int place = atomicAdd(&count[buf], 1);
-                if (place < kList) list[place] = top_key(x[q].get(e), v);
-              }
-            }
-          }
-        }
-      }
-    }
-    __syncthreads();
-    Stats t{m, 0.f, 0.f};
-    t.s = all_sum<NW>(wsum);
-    t.w = all_sum<NW>(wdot);
-    if (m == -INFINITY) t.s = t.w = 0.f;
-    const auto answer = [&](int k, unsigned long long key, const Stats& t, float ls) {
-      a.top_id[(i64)r * a.top + k] = key_token(key);
-      a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value((unsigned)(key >> 32)), t, ls);
-    };
-    const float ls = log_sum(t);
-    if (threadIdx.x == 0) {
-      if (cluster == 1) write_row(a, row, r, t);
-      else part[buf] = t;
-    }
-    const auto own = [&](int c) {              // how many alternatives block c of the cluster can have
-      const int per = (at.vecs + cluster - 1) / cluster, l = c * per, h = min(at.vecs, l + per);
-      return min(a.top, max(0, min(a.V, h * E - at.skip) - max(0, l * E - at.skip)));
-    };
-    if (a.top > 0) {
-      const int have = own(rank), found = count[buf];
-      const auto keep = [&](int k, unsigned long long key) {
-        if (cluster == 1) answer(k, key, t, ls);
-        else best[buf][k] = key;
-      };
-      if (m == m && found <= kList) {
-        by_rank<NT>(list, found, have, keep);
-      } else {
-        unsigned long long last = ~0ull;
-        for (int k = 0; k < have; ++k) {
-          unsigned long long high = 0;
-#pragma unroll
-          for (int q = 0; q < kVecs; ++q) {
-            if (q * NT + threadIdx.x < n) {
-#pragma unroll
-              for (int e = 0; e < E; ++e) {
-                const int v = (lo + q * NT + (int)threadIdx.x) * E + e - at.skip;
-                const unsigned long long key = top_key(x[q].get(e), v);
-                if (v >= 0 && v < a.V && key < last && key > high) high = key;
-              }
-            }
-          }
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o);
-            high = other > high ? other : high;
-          }
-          __syncthreads();
-          if (lane == 0) list[warp] = high;
-          __syncthreads();
-          last = list[0];
-#pragma unroll
-          for (int q = 1; q < NW; ++q) last = list[q] > last ? list[q] : last;
-          if (threadIdx.x == 0) keep(k, last);
-        }
-      }
-    }
-    if (cluster > 1) {
-      // the first block joins what the others have found, while they go on to the next row
-      cg::cluster_group all = cg::this_cluster();
-      all.sync();
-      if (rank == 0) {
-        // a lane fetches a block's statistics, a thread one alternative: one trip to the other blocks, not one for each
-        t = lane < cluster ? *all.map_shared_rank(&part[buf], lane) : Stats{-INFINITY, 0.f, 0.f};
-#pragma unroll
-        for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
-          const Stats b{__shfl_down_sync(0xffffffffu, t.m, o), __shfl_down_sync(0xffffffffu, t.s, o), __shfl_down_sync(0xffffffffu, t.w, o)};
-          t = joined(t, b);
-        }
-        t = Stats{__shfl_sync(0xffffffffu, t.m, 0), __shfl_sync(0xffffffffu, t.s, 0), __shfl_sync(0xffffffffu, t.w, 0)};
-        // (places without an alternative hold zero, below every key)
-        const int total = cluster * a.top;
-        for (int k = threadIdx.x; k < total; k += NT) {
-          const int c = k / a.top;
-          list[k] = k - c * a.top < own(c) ? all.map_shared_rank(best[buf], c)[k - c * a.top] : 0ull;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) write_row(a, row, r, t);
-        const float ls = log_sum(t);
-        by_rank<NT>(list, total, a.top, [&](int k, unsigned long long key) { answer(k, key, t, ls); });
+        for (int e = 0; e < E / 2; ++e) t.add<true>(x[q].pair(e), kLog2e);
       }
     }
   }
-  if (cluster > 1) cg::this_cluster().sync();  // nobody leaves while its shared memory may be read
+  if (p.edge >= 0) see_edge<true, T>(t, edge, kLog2e);
+  float m = warp_max(t.m);
+  if (lane == 0) wmax[warp] = m;
+  const int j = TOP ? (a.top + NW - 1) / NW : 0;
+  if (TOP) {
+    unsigned k = value_key(t.m), b = 0u;
+    for (int i = 0; i < min(j, 32); ++i) {
+      b = __reduce_max_sync(0xffffffffu, k);
+      const unsigned who = __ballot_sync(0xffffffffu, k == b);
+      if (lane == __ffs(who) - 1) k = 0u;
+      if (lane == 0) named[warp * j + i] = b;
+    }
+  }
+  __syncthreads();
+  m = all_max<NW>(wmax);
+  const float m0 = ref_of(m), d = (t.r - m0) * kLog2e, f = ex2(d);
+  const float s1 = warp_sum((t.s.x[0] + t.s.x[1]) * f), w1 = warp_sum(f == 0.f ? 0.f : f * (fmaf(t.s.x[0], d, t.w.x[0]) + fmaf(t.s.x[1], d, t.w.x[1])));
+  if (lane == 0) { wsum[warp] = s1; wdot[warp] = w1; }
+  if (TOP) {
+    unsigned bound = 0u;
+    if (a.top <= 32) {
+      const unsigned mine = lane < NW * j ? named[lane] : 0u;
+      int above = 0;
+#pragma unroll 8
+      for (int i = 0; i < 32; ++i) {
+        const unsigned o = __shfl_sync(0xffffffffu, mine, i);
+        above += o > mine || (o == mine && i < lane);
+      }
+      bound = __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, above == a.top - 1)) - 1);
+    } else {
+      bound = 0xffffffffu;
+      for (int i = lane; i < NW * j; i += 32) bound = min(bound, named[i]);
+      bound = __reduce_min_sync(0xffffffffu, bound);
+    }
+    const float least = bound == 0u ? -INFINITY : key_value(bound);
+    const auto offer = [&](float x, int v) {
+      if (x >= least) {
+        const int place = atomicAdd(&count, 1);
+        if (place < kList) list[place] = top_key(x, v);
+      }
+    };
+    if (p.edge >= 0) offer(edge, p.edge);
+    if (high >= least) {
+      const bool all = others >= least;
+      for (int i = all ? (int)threadIdx.x : where; i < p.n; i += kRow * kBatch) {
+        V16<T> x[kBatch];
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q)
+          if (i + q * kRow < p.n) x[q].w = __ldg(p.first + i + q * kRow);
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+          if (i + q * kRow < p.n && max_of(x[q]) >= least) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) offer(x[q].get(e), p.v0 + (i + q * kRow) * E + e);
+          }
+        }
+        if (!all) break;
+      }
+    }
+  }
+  __syncthreads();
+  Stats all{m, all_sum<NW>(wsum), all_sum<NW>(wdot)};
+  if (m == -INFINITY) all.s = all.w = 0.f;
+  const auto answer = [&](int k, unsigned long long key, const Stats& t, float ls) {
+    a.top_id[(i64)r * a.top + k] = key_token(key);
+    a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value((unsigned)(key >> 32)), t, ls);
+  };
+  const float ls = log_sum(all);
+  if (threadIdx.x == 0) {
+    if (cluster == 1) write_row(a, row, r, all);
+    else part = all;
+  }
+  if (TOP) {
+    const int have = min(a.top, elements_of(row, a.V, cluster, rank)), found = count;
+    const auto keep = [&](int k, unsigned long long key) {
+      if (cluster == 1) answer(k, key, all, ls);
+      else best[k] = key;
+    };
+    if (m == m && found <= kList) {
+      by_rank<kRow>(list, found, have, keep);
+    } else {
+      unsigned long long last = ~0ull;
+      for (int k = 0; k < have; ++k) {
+        unsigned long long top = 0;
+        const auto look = [&](float x, int v) {
+          const unsigned long long key = top_key(x, v);
+          if (key < last && key > top) top = key;
+        };
+        if (p.edge >= 0) look(edge, p.edge);
+        for (int i = threadIdx.x; i < p.n; i += kRow) {
+          V16<T> x;
+          x.w = __ldg(p.first + i);
+#pragma unroll
+          for (int e = 0; e < E; ++e) look(x.get(e), p.v0 + i * E + e);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
+          top = other > top ? other : top;
+        }
+        __syncthreads();
+        if (lane == 0) list[warp] = top;
+        __syncthreads();
+        last = list[0];
+#pragma unroll
+        for (int q = 1; q < NW; ++q) last = list[q] > last ? list[q] : last;
+        if (threadIdx.x == 0) keep(k, last);
+      }
+    }
+  }
+  if (cluster == 1) return;
+  // the first block joins what the others have found: a lane fetches a block's statistics, a thread one alternative
+  cg::cluster_group blocks = cg::this_cluster();
+  blocks.sync();
+  if (rank == 0) {
+    all = lane < cluster ? *blocks.map_shared_rank(&part, lane) : Stats{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+      const Stats b{__shfl_down_sync(0xffffffffu, all.m, o), __shfl_down_sync(0xffffffffu, all.s, o), __shfl_down_sync(0xffffffffu, all.w, o)};
+      all = joined(all, b);
+    }
+    all = Stats{__shfl_sync(0xffffffffu, all.m, 0), __shfl_sync(0xffffffffu, all.s, 0), __shfl_sync(0xffffffffu, all.w, 0)};
+    if (threadIdx.x == 0) write_row(a, row, r, all);
+    if (TOP) {
+      const int total = cluster * a.top;       // (places without an alternative hold zero, below every key)
+      for (int k = threadIdx.x; k < total; k += kRow) {
+        const int c = k / a.top;
+        list[k] = k - c * a.top < elements_of(row, a.V, cluster, c) ? blocks.map_shared_rank(best, c)[k - c * a.top] : 0ull;
+      }
+      __syncthreads();
+      const float ls = log_sum(all);
+      by_rank<kRow>(list, total, a.top, [&](int k, unsigned long long key) { answer(k, key, all, ls); });
+    }
+  }
+  blocks.sync();                               // nobody leaves while its shared memory may be read
 }
 
 // ---- log probabilities of short rows -----------------------------------------------------------------------------------------------
@@ -468,144 +452,65 @@ __global__ void __launch_bounds__(kShortThreads) logprob_short_kernel(const T* _
   }
 }
 
-// ---- log probabilities of rows beyond a cluster's registers -------------------------------------------------------------------------
-
-constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
-
-// sum of v over the block, the same bits in every thread
-__device__ __forceinline__ float block_sum(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float s = 0.f;
-#pragma unroll
-  for (int w = 0; w < kRowWarps; ++w) s += red[w];
-  return s;
-}
-__device__ __forceinline__ float block_max(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float s = red[0];
-#pragma unroll
-  for (int w = 1; w < kRowWarps; ++w) s = max_nan(s, red[w]);
-  return s;
-}
-
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) logprob_wide_kernel(const T* __restrict__ logits, const LogprobArgs a) {
-  __shared__ float red[kRowWarps];
-  __shared__ unsigned long long best[kRowWarps];
-  const int r = blockIdx.x;
-  pdl_wait();
-  pdl_trigger();
-  const T* x = logits + (i64)r * a.ld;
-  float m = -INFINITY;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = max_nan(m, to_f32(x[v]));
-  m = block_max(m, red);
-  const float m0 = ref_of(m);
-  Stats t{m, 0.f, 0.f};
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-    const float e = fmaxf((to_f32(x[v]) - m0) * kLog2e, -150.f), y = ex2(e);
-    t.s += y;
-    t.w = fmaf(y, e, t.w);
-  }
-  t.s = block_sum(t.s, red);
-  t.w = block_sum(t.w, red);
-  if (m == -INFINITY) t.s = t.w = 0.f;
-  if (threadIdx.x == 0) write_row(a, x, r, t);
-  const float ls = log_sum(t);
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < a.top; ++k) {
-    unsigned long long mine = 0;
-    for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-      const unsigned long long q = top_key(to_f32(x[v]), v);
-      if (q < last && q > mine) mine = q;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const unsigned long long q = __shfl_xor_sync(0xffffffffu, mine, o);
-      mine = q > mine ? q : mine;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) best[threadIdx.x >> 5] = mine;
-    __syncthreads();
-    last = best[0];
-    for (int q = 1; q < kRowWarps; ++q) last = best[q] > last ? best[q] : last;
-    if (threadIdx.x == 0) {
-      const int v = key_token(last);
-      a.top_id[(i64)r * a.top + k] = v;
-      a.top_logprob[(i64)r * a.top + k] = logprob_of(to_f32(x[v]), t, ls);
-    }
-  }
-}
-
 // ---- gradient of log probabilities and entropies -----------------------------------------------------------------------------------
 
 struct LogprobGradArgs {
   int N, V; i64 ld, dld;
   const int32_t* tokens; const float *lse, *entropy, *dlogprob, *dentropy;
 };
-constexpr int kGradThreads = 256, kGradVecs = 4;
 
 // Statistics are given, so every element is on its own: a block has a part of a row, all of its loads in flight at once.
 template <class T>
-__global__ void __launch_bounds__(kGradThreads) logprob_back_kernel(const T* logits, T* dlogits, const LogprobGradArgs a, int parts) {
+__global__ void __launch_bounds__(kRow) logprob_back_kernel(const T* logits, T* dlogits, const LogprobGradArgs a, int parts) {
   constexpr int E = V16<T>::E;
-  const int r = blockIdx.x / parts, lo = (blockIdx.x - r * parts) * (kGradThreads * kGradVecs);
+  const int r = blockIdx.x / parts, rank = blockIdx.x - r * parts;
   pdl_wait();
   pdl_trigger();
   const T* row = logits + (i64)r * a.ld;
   T* out = dlogits + (i64)r * a.dld;
-  const RowAt<const T> at(row, a.V);
-  const RowAt<T> to(out, a.V);
-  V16<T> x[kGradVecs];
+  const Part<T> p(row, a.V, parts, rank);
+  V16<T> x[kBatch];
 #pragma unroll
-  for (int q = 0; q < kGradVecs; ++q) {
-    const int i = lo + q * kGradThreads + threadIdx.x;
-    if (i < at.vecs) x[q] = load_vec<T>(row, at, i, a.V);
-  }
+  for (int q = 0; q < kBatch; ++q)
+    if ((int)threadIdx.x + q * kRow < p.n) x[q].w = __ldcs(p.first + threadIdx.x + q * kRow);
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : 0.f;
   const int tok = a.tokens ? a.tokens[r] : -1;
   const bool has = tok >= 0 && tok < a.V;
   const float gl = has ? a.dlogprob[r] : 0.f, ge = a.dentropy ? a.dentropy[r] : 0.f, ent = a.dentropy ? a.entropy[r] : 0.f, lse = a.lse[r];
   const bool dead = lse == -INFINITY;
   const float c0 = fmaf(ge, ent, gl);          // gradient: -p (gl + ge (log p + ent)), and gl at the token
+  const auto one = [&](float v, int at) {
+    const float logp = v - lse, q = ex2(logp * kLog2e), g = q == 0.f ? 0.f : -q * fmaf(ge, logp, c0);
+    return dead ? 0.f : at == tok ? g + gl : g;
+  };
+  const bool same = (((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0;
 #pragma unroll
-  for (int q = 0; q < kGradVecs; ++q) {
-    const int i = lo + q * kGradThreads + threadIdx.x;
-    if (i < at.vecs) {
+  for (int q = 0; q < kBatch; ++q) {
+    const int i = (int)threadIdx.x + q * kRow, v = p.v0 + i * E;
+    if (i < p.n) {
       V16<T> y;
 #pragma unroll
       for (int e = 0; e < E / 2; ++e) {
         const F<2> logp = x[q].pair(e) + F<2>::all(-lse);
-        const F<2> p = each(logp * F<2>::all(kLog2e), [](float v, int) { return ex2(v); });
-        F<2> g = fma_(logp, F<2>::all(-ge), F<2>::all(-c0)) * p;
-        y.set_pair(e, each(g, [&](float v, int k) { return p.x[k] == 0.f ? 0.f : v; }));
+        const F<2> pr = each(logp * F<2>::all(kLog2e), [](float v, int) { return ex2(v); });
+        const F<2> g = fma_(logp, F<2>::all(-ge), F<2>::all(-c0)) * pr;
+        y.set_pair(e, each(g, [&](float v, int k) { return pr.x[k] == 0.f ? 0.f : v; }));
       }
       if (dead) y.w = make_uint4(0u, 0u, 0u, 0u);
-      if (has && !dead && tok + at.skip >= i * E && tok + at.skip < i * E + E) {
+      if (has && (unsigned)(tok - v) < (unsigned)E) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (i * E + e - at.skip == tok) {
-            const float logp = x[q].get(e) - lse, p = ex2(logp * kLog2e);
-            y.set(e, (p == 0.f ? 0.f : -p * fmaf(ge, logp, c0)) + gl);
-          }
+          if (v + e == tok) y.set(e, one(x[q].get(e), tok));
       }
-      if (i > 0 && i + 1 < at.vecs && to.skip == at.skip) {
-        *(reinterpret_cast<uint4*>(to.base) + i) = y.w;
+      if (same) {
+        __stcs(reinterpret_cast<uint4*>(out + v), y.w);
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int v = i * E + e - at.skip;
-          if (v >= 0 && v < a.V) out[v] = y.raw(e);
-        }
+        for (int e = 0; e < E; ++e) out[v + e] = y.raw(e);
       }
     }
   }
+  if (p.edge >= 0) out[p.edge] = from_f32<T>(one(edge, p.edge));
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------------------------
@@ -617,212 +522,161 @@ struct DistillArgs {
 // The student's side of one row: q = 2^((x - m) c) / s with c = log2(e) / tau
 struct Student { float m, s; };
 
-// A block, or a cluster, has a row in its registers (see above).  The gradient of the whole row is scale q; the places of the teacher's
-// alternatives are written once more, by the first of those that name the same token, after the block has written the rest.
-template <class T, int NT>
-__global__ void __launch_bounds__(NT, 512 / NT) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
-  constexpr int E = V16<T>::E, NW = NT / 32;
-  extern __shared__ uint4 staged[];
-  __shared__ float prob[2][kMaxTeacher];       // teacher: logit / tau, then probability (rows in turn: a slow warp may still read the last one's)
-  __shared__ float gap[2][kMaxTeacher];        // student's logit
-  __shared__ int id[2][kMaxTeacher];
+// Two passes over a row, the second from L2.  The gradient of the whole row is scale q; the places of the teacher's alternatives are written
+// once more, by the first of those that name the same token, after the block has written the rest.
+template <class T>
+__global__ void __launch_bounds__(kRow, 4) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
+  constexpr int E = V16<T>::E, NW = kRow / 32;
+  extern __shared__ float teacher[];           // [K] logit / tau, then probability; [K] the student's logit; [K] token
+  float *prob = teacher, *gap = prob + a.K;
+  int* id = reinterpret_cast<int*>(gap + a.K);
   __shared__ float wm[NW], wy[NW], wany[NW], wsum[NW], wmass[NW], wloss[NW];
-  __shared__ Student part[2];
-  const int rank = blockIdx.x % cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.x / cluster;
+  __shared__ Student part;
+  const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  const Stage<T, NT> stage{logits, logits + ((i64)(a.N - 1) * a.ld + a.V), a.ld, a.V, cluster, rank, staged + threadIdx.x};
-  const float inv = 1.0f / a.tau, c = kLog2e * inv, uniform = 1.0f / (float)a.N;
-  int r = blockIdx.x / cluster;
-  if (r < a.N) stage.bring(r);
-  copies_issued();
-  // The thread's first alternative is fetched ahead: its token and logit two rows, the student's logit of that token one row.
-  struct Teacher { int v; float y, z; };
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const Part<T> p(row, a.V, cluster, rank);
+  const float inv = 1.0f / a.tau, c = kLog2e * inv;
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
+  const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
   const bool teaches = warp * 32 < a.K;        // (the other warps have no alternatives)
-  const auto named = [&](int row, int k) {
-    Teacher t{-1, -INFINITY, -INFINITY};
-    if (row < a.N && k < a.K) {
-      t.v = a.top_id[(i64)row * a.K + k];
-      t.y = a.top_logit[(i64)row * a.K + k];
-    }
-    return t;
-  };
-  const auto look_up = [&](Teacher& t, int row) {
-    if (t.v >= 0 && t.v < a.V) t.z = to_f32(logits[(i64)row * a.ld + t.v]);
-    else t.v = -1;
-  };
-  const auto weight_of = [&](int row) { return a.weight ? a.weight[min(row, a.N - 1)] : uniform; };
-  Teacher now{-1, -INFINITY, -INFINITY}, soon = now;
-  if (teaches) {
-    now = named(r, threadIdx.x);
-    look_up(now, r);
-    soon = named(r + step, threadIdx.x);
+  for (int k = threadIdx.x; k < a.K; k += kRow) {
+    const int v = a.top_id[(i64)r * a.K + k];
+    const bool in = v >= 0 && v < a.V;
+    id[k] = in ? v : -1;
+    prob[k] = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
   }
-  float next_weight = weight_of(r);
-  // Elements of vectors that the row only has a part of, written one by one by the last warp: lanes 0.. those of its first vector, lanes
-  // 16.. those of its last one; the logits are fetched a row ahead.
-  const auto edge_of = [&](int row) {
-    if (warp != NW - 1 || row >= a.N || (lane & 15) >= E) return -1;
-    const RowAt<const T> at(logits + (i64)row * a.ld, a.V);
-    const int per = stage.share(at), e = lane & 15, v = (lane < 16 ? 0 : (at.vecs - 1) * E) + e - at.skip;
-    if (v < 0 || v >= a.V) return -1;
-    const bool partial = lane < 16 ? at.skip > 0 : at.vecs * E > a.V + at.skip;
-    const int owner = (lane < 16 ? 0 : at.vecs - 1) / per;
-    return partial && owner == rank ? v : -1;
-  };
-  int edge = edge_of(r);
-  float edge_logit = edge >= 0 ? to_f32(logits[(i64)r * a.ld + edge]) : 0.f;
-  for (int buf = 0; r < a.N; r += step, buf ^= 1) {
-    const T* row = logits + (i64)r * a.ld;
-    T* out = dlogits + (i64)r * a.dld;
-    const float weight = next_weight;
-    next_weight = weight_of(r + step);
-    float ym = -INFINITY;
-    bool any = false;
-    if (teaches) {
-      for (int k = threadIdx.x; k < a.K; k += NT) {
-        Teacher t = now;
-        if (k >= NT) {
-          t = named(r, k);
-          look_up(t, r);
-        }
-        const float y = t.v >= 0 ? t.y * inv : -INFINITY;
-        id[buf][k] = t.v;
-        prob[buf][k] = y;
-        gap[buf][k] = t.v >= 0 ? t.z : -INFINITY;
-        ym = fmaxf(ym, y);                     // (a NaN shows in the sum)
-        any = any || y != -INFINITY;
-      }
-      now = soon;
-      look_up(now, r + step);
-      soon = named(r + 2 * step, threadIdx.x);
-      ym = warp_max(ym);
-      any = __any_sync(0xffffffffu, any);
-    }
-    V16<T> x[kVecs];
-    int lo;
-    const int n = stage.take(r, x, lo);
-    if (r + step < a.N) stage.bring(r + step);
-    copies_issued();
-    const RowAt<const T> at(row, a.V);
-    const RowAt<T> to(out, a.V);
+  Seen t;
+  for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * kRow < p.n) x[q].w = p.first[i + q * kRow];
     float m = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < kVecs; ++q)
-      if (q * NT + threadIdx.x < n) m = max_nan(m, max_of(x[q]));
-    m = warp_max(m);
-    if (lane == 0) { wm[warp] = m; wy[warp] = ym; wany[warp] = any ? 1.f : 0.f; }
-    __syncthreads();
-    m = all_max<NW>(wm);
-    ym = all_max<NW>(wy);
-    const float present = all_max<NW>(wany);
-    const float m0 = ref_of(m), y0 = ref_of(ym);
-    const F<2> scale = F<2>::all(c);
-    F<2> sum = F<2>::all(0.f);
-    float mass = 0.f;
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * kRow < p.n) m = max_nan(m, max_of(x[q]));
+    t.follow(m, c);
 #pragma unroll
-    for (int q = 0; q < kVecs; ++q) {
-      if (q * NT + threadIdx.x < n) {
+    for (int q = 0; q < kBatch; ++q) {
+      if (i + q * kRow < p.n) {
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) sum = sum + each((x[q].pair(e) + F<2>::all(-m0)) * scale, [](float v, int) { return ex2(v); });
-      }
-    }
-    if (teaches) {
-      for (int k = threadIdx.x; k < a.K; k += NT) mass += ex2((prob[buf][k] - y0) * kLog2e);
-      mass = warp_sum(mass);
-    }
-    float s = warp_sum(sum.x[0] + sum.x[1]);
-    if (lane == 0) { wsum[warp] = s; wmass[warp] = mass; }
-    __syncthreads();
-    s = all_sum<NW>(wsum);
-    float M = m0;
-    if (cluster > 1) {
-      cg::cluster_group all = cg::this_cluster();
-      if (threadIdx.x == 0) part[buf] = Student{m, s};
-      all.sync();                              // (also: every block has read what it needs before the first gradient is written)
-      const Student b = lane < cluster ? *all.map_shared_rank(&part[buf], lane) : Student{-INFINITY, 0.f};      // (one trip for all)
-      M = ref_of(warp_max(b.m));
-      s = warp_sum(b.s == 0.f ? 0.f : b.s * ex2((b.m - M) * c));
-    }
-    const float gain = weight * a.tau;
-    float loss = 0.f;
-    if (teaches) {
-      const float ls = logf(s), lmass = logf(all_sum<NW>(wmass));
-      for (int k = threadIdx.x; k < a.K; k += NT) {
-        const float logp = (prob[buf][k] - y0) - lmass, p = ex2(logp * kLog2e), z = gap[buf][k];
-        const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
-        loss += p == 0.f ? 0.f : p * (logp - logq);
-        prob[buf][k] = p;
-      }
-      loss = warp_sum(loss);
-    }
-    if (lane == 0) wloss[warp] = loss;
-    const bool none = present == 0.f || weight == 0.f;
-    const F<2> f = F<2>::all(s == 0.f ? 0.f : gain / s), from = F<2>::all(-M);
-    const int whole_from = lo == 0 && at.skip > 0 ? 1 : 0;      // vectors that are the row's alone
-    const int left = n - (lo + n == at.vecs && at.vecs * E > a.V + at.skip ? 1 : 0) - (int)threadIdx.x;
-    if (to.skip == at.skip) {
-      uint4* dst = reinterpret_cast<uint4*>(to.base) + lo + threadIdx.x;
-      if (!none) {
-#pragma unroll
-        for (int q = 0; q < kVecs; ++q) {
-          if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) {
-            V16<T> y;
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) y.set_pair(e, each((x[q].pair(e) + from) * scale, [](float v, int) { return ex2(v); }) * f);
-            __stcs(dst + q * NT, y.w);
-          }
-        }
-      } else {
-#pragma unroll 1
-        for (int q = 0; q < kVecs; ++q)
-          if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) __stcs(dst + q * NT, make_uint4(0u, 0u, 0u, 0u));
-      }
-    } else {                                   // rows of the two arrays start at different places of a vector
-#pragma unroll
-      for (int q = 0; q < kVecs; ++q) {
-        if (q * NT < left && !(q == 0 && (int)threadIdx.x < whole_from)) {
-          T* dst = out + (i64)(lo + q * NT + (int)threadIdx.x) * E - at.skip;
-#pragma unroll
-          for (int e = 0; e < E; ++e) dst[e] = from_f32<T>(none ? 0.f : ex2((x[q].get(e) - M) * c) * f.x[0]);
-        }
-      }
-    }
-    if (warp == NW - 1) {
-      if (edge >= 0) out[edge] = from_f32<T>(none ? 0.f : ex2((edge_logit - M) * c) * f.x[0]);
-      edge = edge_of(r + step);
-      edge_logit = edge >= 0 ? to_f32(logits[(i64)(r + step) * a.ld + edge]) : 0.f;
-    }
-    __syncthreads();
-    if (rank == 0 && warp == NW - 1) {
-      const float t = all_sum<NW>(wloss);
-      if (lane == 0) a.row_loss[r] = present != 0.f ? a.tau * a.tau * t : 0.f;
-    }
-    if (!none && teaches) {
-      const int begin = lo * E - at.skip, stop = (lo + n) * E - at.skip;      // the block's own tokens
-      for (int k0 = warp * 32; k0 < a.K; k0 += NT) {
-        const int k = k0 + lane, v = k < a.K ? id[buf][k] : -1;
-        float p = k < a.K ? prob[buf][k] : 0.f;
-        bool first = true;
-        const int namesakes = __popc(__match_any_sync(0xffffffffu, v));      // (every lane takes part)
-        if (a.K > 32 || __any_sync(0xffffffffu, v >= 0 && namesakes > 1)) {
-          // the same token may be named twice: its first place adds all of them up, in their order
-          p = 0.f;
-#pragma unroll 4
-          for (int j = 0; j < a.K; ++j) {
-            const bool same = id[buf][j] == v;
-            first = first && !(same && j < k);
-            p += same ? prob[buf][j] : 0.f;
-          }
-        }
-        if (v >= 0 && v >= begin && v < stop && first) {
-          const float q = s == 0.f ? 0.f : ex2((gap[buf][k] - M) * c) / s;
-          out[v] = from_f32<T>(gain * (q - p));
-        }
+        for (int e = 0; e < E / 2; ++e) t.add<false>(x[q].pair(e), c);
       }
     }
   }
-  if (cluster > 1) cg::this_cluster().sync();  // nobody leaves while its shared memory may be read
+  if (p.edge >= 0) see_edge<false, T>(t, edge, c);
+  float ym = -INFINITY;
+  bool any = false;
+  for (int k = threadIdx.x; k < a.K; k += kRow) {
+    gap[k] = id[k] >= 0 ? to_f32(row[id[k]]) : -INFINITY;
+    ym = fmaxf(ym, prob[k]);                   // (a NaN shows in the sum)
+    any = any || prob[k] != -INFINITY;
+  }
+  float m = warp_max(t.m);
+  ym = warp_max(ym);
+  any = __any_sync(0xffffffffu, any);
+  if (lane == 0) { wm[warp] = m; wy[warp] = ym; wany[warp] = any ? 1.f : 0.f; }
+  __syncthreads();
+  m = all_max<NW>(wm);
+  ym = all_max<NW>(wy);
+  const float present = all_max<NW>(wany);
+  const float m0 = ref_of(m), y0 = ref_of(ym);
+  float s = warp_sum((t.s.x[0] + t.s.x[1]) * ex2((t.r - m0) * c)), mass = 0.f;
+  if (teaches) {
+    for (int k = threadIdx.x; k < a.K; k += kRow) mass += ex2((prob[k] - y0) * kLog2e);
+    mass = warp_sum(mass);
+  }
+  if (lane == 0) { wsum[warp] = s; wmass[warp] = mass; }
+  __syncthreads();
+  s = all_sum<NW>(wsum);
+  if (m == -INFINITY) s = 0.f;
+  if (m != m || m == INFINITY) s = __int_as_float(0x7fc00000);
+  float M = m0;
+  if (cluster > 1) {
+    cg::cluster_group blocks = cg::this_cluster();
+    if (threadIdx.x == 0) part = Student{m, s};
+    blocks.sync();                             // (also: every block has read what it needs before the first gradient is written)
+    const Student b = lane < cluster ? *blocks.map_shared_rank(&part, lane) : Student{-INFINITY, 0.f};
+    M = ref_of(warp_max(b.m));
+    s = warp_sum(b.s == 0.f ? 0.f : b.s * ex2((b.m - M) * c));
+    blocks.barrier_arrive();                   // (waited for at the end: nobody leaves while its shared memory may be read)
+  }
+  const float gain = weight * a.tau;
+  float loss = 0.f;
+  if (teaches) {
+    const float ls = logf(s), lmass = logf(all_sum<NW>(wmass));
+    for (int k = threadIdx.x; k < a.K; k += kRow) {
+      const float logp = (prob[k] - y0) - lmass, pr = ex2(logp * kLog2e), z = gap[k];
+      const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
+      loss += pr == 0.f ? 0.f : pr * (logp - logq);
+      prob[k] = pr;
+    }
+    loss = warp_sum(loss);
+  }
+  if (lane == 0) wloss[warp] = loss;
+  const bool none = present == 0.f || weight == 0.f;
+  const float f = s == 0.f ? 0.f : gain / s;
+  const auto one = [&](float v) { return none ? 0.f : ex2((v - M) * c) * f; };
+  const bool same = (((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0;
+  if (same && !none) {
+    for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
+      V16<T> x[kBatch];
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q)
+        if (i + q * kRow < p.n) x[q].w = __ldcs(p.first + i + q * kRow);
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        if (i + q * kRow < p.n) {
+          V16<T> y;
+#pragma unroll
+          for (int e = 0; e < E / 2; ++e)
+            y.set_pair(e, each((x[q].pair(e) + F<2>::all(-M)) * F<2>::all(c), [](float v, int) { return ex2(v); }) * F<2>::all(f));
+          __stcs(reinterpret_cast<uint4*>(out + p.v0) + i + q * kRow, y.w);
+        }
+      }
+    }
+  } else {                                     // a row of zeros, or rows that start at different places of a vector
+    for (int i = threadIdx.x; i < p.n; i += kRow) {
+      V16<T> x;
+      x.w = __ldcs(p.first + i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[p.v0 + i * E + e] = from_f32<T>(one(x.get(e)));
+    }
+  }
+  if (p.edge >= 0) out[p.edge] = from_f32<T>(one(edge));
+  __syncthreads();
+  if (rank == 0 && warp == NW - 1) {
+    loss = all_sum<NW>(wloss);
+    if (lane == 0) a.row_loss[r] = present != 0.f ? a.tau * a.tau * loss : 0.f;
+  }
+  if (!none && teaches) {
+    const int begin = p.v0, stop = p.v0 + (int)p.n * E;      // the block's whole vectors
+    for (int k0 = warp * 32; k0 < a.K; k0 += kRow) {
+      const int k = k0 + lane, v = k < a.K ? id[k] : -1;
+      float pr = k < a.K ? prob[k] : 0.f;
+      bool first = true;
+      const int namesakes = __popc(__match_any_sync(0xffffffffu, v));      // (every lane takes part)
+      if (a.K > 32 || __any_sync(0xffffffffu, v >= 0 && namesakes > 1)) {
+        // the same token may be named twice: its first place adds all of them up, in their order
+        pr = 0.f;
+#pragma unroll 4
+        for (int j = 0; j < a.K; ++j) {
+          const bool twin = id[j] == v;
+          first = first && !(twin && j < k);
+          pr += twin ? prob[j] : 0.f;
+        }
+      }
+      const bool own = (v >= begin && v < stop) || (v >= 0 && rank == 0 && v < begin) || (rank == cluster - 1 && v >= stop);
+      if (v >= 0 && own && first) {
+        const float q = s == 0.f ? 0.f : ex2((gap[k] - M) * c) / s;
+        out[v] = from_f32<T>(gain * (q - pr));
+      }
+    }
+  }
+  if (cluster > 1) cg::this_cluster().barrier_wait();
 }
 
 // Short rows: G lanes have a row, PER logits each; the teacher's probabilities of each token meet in shared memory, in the order of the
@@ -911,77 +765,6 @@ __global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* l
   }
 }
 
-// rows beyond a cluster's registers
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) distill_wide_kernel(const T* logits, T* dlogits, const DistillArgs a) {
-  __shared__ float red[kRowWarps];
-  __shared__ float prob[kMaxTeacher];
-  __shared__ int id[kMaxTeacher];
-  __shared__ float logit[kMaxTeacher];
-  const int r = blockIdx.x;
-  const T* x = logits + (i64)r * a.ld;
-  T* d = dlogits + (i64)r * a.dld;
-  const float inv = 1.0f / a.tau;
-  pdl_wait();
-  pdl_trigger();
-  // the teacher
-  float ym = -INFINITY, present = 0.f;
-  for (int k = threadIdx.x; k < a.K; k += kRowThreads) {
-    const int v = a.top_id[(i64)r * a.K + k];
-    const bool in = v >= 0 && v < a.V;
-    const float y = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
-    id[k] = in ? v : -1;
-    prob[k] = y;
-    logit[k] = in ? to_f32(x[v]) * inv : -INFINITY;
-    ym = fmaxf(ym, y);      // (a NaN shows in the sum)
-    if (y != -INFINITY) present = 1.f;
-  }
-  present = block_sum(present, red);
-  const float w = a.weight ? a.weight[r] : 1.0f / (float)a.N;
-  ym = block_max(ym, red);
-  if (ym == -INFINITY) ym = 0.f;
-  float mass = 0.f;
-  for (int k = threadIdx.x; k < a.K; k += kRowThreads) mass += expf(prob[k] - ym);
-  mass = block_sum(mass, red);
-  // the student
-  float m = -INFINITY;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) m = max_nan(m, to_f32(x[v]) * inv);
-  m = block_max(m, red);
-  if (m == -INFINITY) m = 0.f;
-  float s = 0.f;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) s += expf(to_f32(x[v]) * inv - m);
-  s = block_sum(s, red);
-  const float logs = logf(s), logmass = logf(mass);
-  float loss = 0.f;
-  for (int k = threadIdx.x; k < a.K; k += kRowThreads) {
-    const float logp = (prob[k] - ym) - logmass, p = expf(logp), z = logit[k];
-    const float logq = z == -INFINITY ? -INFINITY : (z - m) - logs;
-    loss += p == 0.f ? 0.f : p * (logp - logq);
-    prob[k] = p;
-  }
-  loss = block_sum(loss, red);
-  if (threadIdx.x == 0) a.row_loss[r] = present != 0.f ? a.tau * a.tau * loss : 0.f;
-  const float scale = w * a.tau;
-  const bool none = present == 0.f || w == 0.f;
-  for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-    const float q = s == 0.f ? 0.f : expf(to_f32(x[v]) * inv - m) / s;
-    d[v] = from_f32<T>(none ? 0.f : scale * q);
-  }
-  __syncthreads();
-  for (int k = threadIdx.x; k < a.K && !none; k += kRowThreads) {
-    const int v = id[k];
-    if (v < 0) continue;
-    float p = 0.f;
-    bool again = false;
-    for (int j = 0; j < a.K; ++j) {
-      if (id[j] != v) continue;
-      again = again || j < k;
-      p += prob[j];
-    }
-    if (!again) d[v] = from_f32<T>(scale * ((s == 0.f ? 0.f : expf(logit[k] - m) / s) - p));
-  }
-}
-
 __global__ void __launch_bounds__(1024) distill_loss_kernel(int N, const float* __restrict__ row_loss, const float* __restrict__ weight, float* __restrict__ loss) {
   __shared__ float part[32];
   pdl_wait();
@@ -1012,38 +795,20 @@ int launched(cudaError_t e) {
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
-// Blocks that share a row of `vecs` vectors, and their threads.  The fewest that hold it, 64 threads where they suffice; where that leaves
-// SMs without work, more of them, down to two vectors a thread (8 rows of 131072 in bf16: 21 us on 32 blocks, 9 on 128).  0: too long.
-struct Split { int cluster, threads; };
-Split split_of(int N, i64 vecs) {
-  if (vecs > (i64)kMaxCluster * 512 * kVecs) return {0, 0};
-  if (vecs <= 64 * kVecs && (i64)N * ((vecs + 255) / 256) >= 296) return {1, 64};
+// Blocks that share a row: one for about 64 KB of it; more of them, down to 8 KB each, where that leaves SMs without work.
+int blocks_of(int N, i64 bytes) {
   int c = 1;
-  const int threads = vecs <= 256 * kVecs ? 256 : 512;
-  while ((vecs + c - 1) / c > threads * kVecs) c *= 2;
-  while (c < kMaxCluster && (i64)N * c < 148 && vecs / (2 * c) >= 1024) c *= 2;
-  return {c, (vecs + c - 1) / c <= 256 * kVecs ? 256 : 512};
+  while (c < kMaxCluster && bytes > c * (i64)65536) c *= 2;
+  while (c < kMaxCluster && (i64)N * c < 148 && bytes >= 2 * c * (i64)8192) c *= 2;
+  return c;
 }
-// Blocks stay for several rows, each with the next one on its way.
-template <class K, class T, class... Args> cudaError_t launch_rows(K kern, int N, Split sp, cudaStream_t s, int (&known)[kMaxDevices], const T* x, Args&&... args) {
-  const int dev = current_device_slot(), smem = kVecs * sp.threads * 16;
-  if (dev < 0) return cudaErrorInvalidDevice;
-  if (!known[dev]) {
-    int per_sm = 0, sms = 0;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, sp.threads, smem);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess || per_sm * sms == 0) return e != cudaSuccess ? e : cudaErrorInvalidConfiguration;
-    known[dev] = per_sm * sms;
+template <class... KArgs, class... Args>
+cudaError_t launch_rows(void (*kern)(KArgs...), int N, int cluster, size_t smem, cudaStream_t s, Args&&... args) {
+  if (cluster > 8) {                           // more than the portable size
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
   }
-  const int most = known[dev] / sp.cluster, groups = N < most ? N : most;
-  return launch_pdl_cluster(kern, sp.cluster, dim3((unsigned)(groups * sp.cluster)), dim3(sp.threads), (size_t)smem, s, x, static_cast<Args&&>(args)..., sp.cluster);
-}
-// vectors of a row; one more where rows start inside a vector
-i64 vecs_of(int V, int dtype, const void* p, i64 ld) {
-  const i64 es = (i64)elem_size(dtype);
-  return (V * es + 15) / 16 + ((((uintptr_t)p | (uintptr_t)(ld * es)) & 15u) ? 1 : 0);
+  return launch_pdl_cluster(kern, cluster, dim3((unsigned)N * (unsigned)cluster), dim3(kRow), smem, s, static_cast<Args&&>(args)..., cluster);
 }
 
 }  // namespace
@@ -1058,7 +823,7 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
   if (rc != MGRIT_OK) return rc;
   if (top < 0 || top > V || (top > 0 && N > 0 && (!top_logprob || !top_id)) || (tokens && !logprob)) return MGRIT_INVALID_ARG;
   if (!aligned4(tokens) || !aligned4(logprob) || !aligned4(entropy) || !aligned4(lse) || !aligned4(top_logprob) || !aligned4(top_id)) return MGRIT_INVALID_ARG;
-  if (top > kMaxTop) return MGRIT_UNSUPPORTED;
+  if (top > kMaxTop || N > INT32_MAX / kMaxCluster) return MGRIT_UNSUPPORTED;
   if (N == 0) return MGRIT_OK;
   cudaError_t e = cudaSuccess;
   const LogprobArgs a{N, V, top, ld, tokens, logprob, entropy, lse, top_logprob, top_id};
@@ -1066,16 +831,13 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
     using T = decltype(tag);
     const T* x = static_cast<const T*>(logits);
     cudaStream_t s = (cudaStream_t)stream;
-    const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
-    static int known[3][kMaxDevices];          // resident blocks of the three kernels, by device
+    const int c = blocks_of(N, (i64)V * (i64)sizeof(T));
     const auto few = [&](auto kern, int lanes) { e = launch_pdl(kern, dim3((unsigned)(((i64)N * lanes + kShortThreads - 1) / kShortThreads)), dim3(kShortThreads), 0, s, x, a); };
     if (V <= 64) few(logprob_short_kernel<T, 8, 8>, 8);
     else if (V <= 256) few(logprob_short_kernel<T, 32, 8>, 32);
     else if (V <= kShortRow) few(logprob_short_kernel<T, 32, 32>, 32);
-    else if (sp.cluster == 0) e = launch_pdl(logprob_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, a);
-    else if (sp.threads == 64) e = launch_rows(logprob_kernel<T, 64>, N, sp, s, known[0], x, a);
-    else if (sp.threads == 256) e = launch_rows(logprob_kernel<T, 256>, N, sp, s, known[1], x, a);
-    else e = launch_rows(logprob_kernel<T, 512>, N, sp, s, known[2], x, a);
+    else if (top > 0) e = launch_rows(logprob_kernel<T, true>, N, c, 0, s, x, a);
+    else e = launch_rows(logprob_kernel<T, false>, N, c, 0, s, x, a);
   });
   return launched(e);
 }
@@ -1091,13 +853,13 @@ int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* log
   if (N == 0) return MGRIT_OK;
   if (!lse || !tokens != !dlogprob || !entropy != !dentropy || (!tokens && !entropy)) return MGRIT_INVALID_ARG;
   if (dlogits == logits && dld != ld && N > 1) return MGRIT_INVALID_ARG;
-  const i64 parts = (vecs_of(V, dtype, logits, ld) + kGradThreads * kGradVecs - 1) / (kGradThreads * kGradVecs);
+  const i64 parts = ((i64)V * (i64)elem_size(dtype) / 16 + kRow * kBatch - 1) / (kRow * kBatch) + (V * (i64)elem_size(dtype) < 16);
   if (N * parts >= INT32_MAX) return MGRIT_UNSUPPORTED;
   cudaError_t e = cudaSuccess;
   const LogprobGradArgs a{N, V, ld, dld, tokens, lse, entropy, dlogprob, dentropy};
   with_elem(dtype, [&](auto tag) {
     using T = decltype(tag);
-    e = launch_pdl(logprob_back_kernel<T>, dim3((unsigned)(N * parts)), dim3(kGradThreads), 0, (cudaStream_t)stream, static_cast<const T*>(logits), static_cast<T*>(dlogits), a,
+    e = launch_pdl(logprob_back_kernel<T>, dim3((unsigned)(N * parts)), dim3(kRow), 0, (cudaStream_t)stream, static_cast<const T*>(logits), static_cast<T*>(dlogits), a,
                    (int)parts);
   });
   return launched(e);
@@ -1111,7 +873,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
   if (rc == MGRIT_OK) rc = check_logits(N, V, dtype, dlogits, dld);
   if (rc != MGRIT_OK) return rc;
   if (K < 1 || !(tau > 0.f) || tau > 3.0e38f || 1.0f / tau > 3.0e38f || !loss || !aligned4(loss)) return MGRIT_INVALID_ARG;
-  if (K > kMaxTeacher) return MGRIT_UNSUPPORTED;
+  if (K > kMaxTeacher || N > INT32_MAX / kMaxCluster) return MGRIT_UNSUPPORTED;
   cudaStream_t s = (cudaStream_t)stream;
   if (N > 0) {
     if (!top_id || !top_logit || !row_loss || (dlogits == logits && dld != ld && N > 1)) return MGRIT_INVALID_ARG;
@@ -1123,8 +885,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
       using T = decltype(tag);
       const T* x = static_cast<const T*>(logits);
       T* d = static_cast<T*>(dlogits);
-      const Split sp = split_of(N, vecs_of(V, dtype, logits, ld));
-      static int known[3][kMaxDevices];        // resident blocks of the three kernels, by device
+      const int c = blocks_of(N, (i64)V * (i64)sizeof(T));
       const auto few = [&](auto kern, int lanes) {
         const i64 blocks = ((i64)N * lanes + kShortThreads - 1) / kShortThreads;
         added = blocks == 1;
@@ -1133,10 +894,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
       if (V <= 64) few(distill_short_kernel<T, 8, 8>, 8);
       else if (V <= 256) few(distill_short_kernel<T, 32, 8>, 32);
       else if (V <= kShortRow) few(distill_short_kernel<T, 32, 32>, 32);
-      else if (sp.cluster == 0) e = launch_pdl(distill_wide_kernel<T>, dim3(N), dim3(kRowThreads), 0, s, x, d, a);
-      else if (sp.threads == 64) e = launch_rows(distill_kernel<T, 64>, N, sp, s, known[0], x, d, a);
-    else if (sp.threads == 256) e = launch_rows(distill_kernel<T, 256>, N, sp, s, known[1], x, d, a);
-      else e = launch_rows(distill_kernel<T, 512>, N, sp, s, known[2], x, d, a);
+      else e = launch_rows(distill_kernel<T>, N, c, (size_t)K * 12, s, x, d, a);
     });
     rc = launched(e);
     if (rc != MGRIT_OK || added) return rc;
