@@ -370,31 +370,39 @@ def xent_head_fwd_bwd_noalloc(hT, Wc, bc, labels, out=None):
 
 # ---- linear recurrences, token probabilities, distillation: arrays of fp32, bf16 or fp16, any strides with contiguous rows ----------
 
-def _require(ok, what):
+def _require(ok, what, *args):
     if not ok:
-        raise ValueError(what)
+        raise ValueError(what.format(*args))
 
 
 def _dtype(t):
     code = _DTYPES.get(t.dtype)
-    _require(code is not None, f"fp32, bf16 or fp16 required, got {t.dtype}")
+    _require(code is not None, "fp32, bf16 or fp16 required, got {}", t.dtype)
     return code
 
 
-def _on_device(dev, fn, *args):
+# the current stream's handle and the current device without the objects around them (7 us of a call that takes 12)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _run(dev, fn, *args):
     """fn(*args, stream) on the current stream of `dev`, whatever device is current."""
-    if torch.cuda.current_device() == dev.index:
-        return _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
-    with torch.cuda.device(dev):
-        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    if _device_now() == dev.index:
+        rc = fn(*args, _stream_of(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream_of(dev.index))
+    if rc != OK:
+        raise MgritError(rc)
 
 
 def _like(t, dev, shape, dtype, name):
     """Address of a contiguous array of that device, shape and type (0: not given)."""
     if t is None:
         return 0
-    _require(t.device == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous(),
-             f"{name}: contiguous {dtype} array of shape {tuple(shape)} on {dev} required")
+    if not (t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == dev):
+        raise ValueError(f"{name}: contiguous {dtype} array of shape {tuple(shape)} on {dev} required")
     return t.data_ptr()
 
 
@@ -402,35 +410,37 @@ def _strided(t, like, name):
     """(address, stride of t, stride of b) of an array of the shape, type and device of `like`."""
     if t is None:
         return 0, 0, 0
-    _require(t.shape == like.shape and t.dtype == like.dtype and t.device == like.device, f"{name}: {like.dtype} array of shape {tuple(like.shape)} on {like.device} required")
-    st = t.stride()
-    _require(st[2] == 1 or t.shape[2] == 1, f"{name}: the units of a row must be contiguous")
-    return t.data_ptr(), st[0], st[1]
+    st, sb, su = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if not (t.shape == like.shape and t.dtype is like.dtype and t.device == like.device and (su == 1 or t.shape[2] == 1)):
+        raise ValueError(f"{name}: {like.dtype} array of shape {tuple(like.shape)} on {like.device} with contiguous units required")
+    return t.data_ptr(), st, sb
 
 
 _SCAN_ARGS = struct.Struct("@5if" + 3 * "Pqq" + "Pqq" + "PPP" + "Pqq" + "P" + 2 * "Pqq" + "P")      # gated_scan_args
 
 
-def _scan_args(gate, cand, h, reset, lengths, h0, cell, dt):
+def _scan_sizes(gate):
     _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
-    T, Bn, H = gate.shape
-    dev = gate.device
-    if reset is not None:
-        _require(reset.dtype in (torch.uint8, torch.bool) and reset.shape == (T, Bn) and reset.device == dev, f"reset: uint8 or bool array [T,B] on {dev} required")
-        r = (reset.data_ptr(), *reset.stride())
-    else:
+    return gate.shape
+
+
+def _scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev):
+    if reset is None:
         r = (0, 0, 0)
-    return (T, Bn, H, cell, _dtype(gate), dt, *_strided(gate, gate, "gate"), *_strided(cand, gate, "cand"), *_strided(h, gate, "h"), *r,
-            _like(h0, dev, (Bn, H), torch.float32, "h0"), _like(lengths, dev, (Bn,), torch.int32, "lengths"))
+    else:
+        _require(reset.dtype in (torch.uint8, torch.bool) and reset.shape == shape[:2] and reset.device == dev, "reset: uint8 or bool array [T,B] on {} required", dev)
+        r = (reset.data_ptr(), *reset.stride())
+    return (*shape, cell, _dtype(gate), dt, *_strided(gate, gate, "gate"), *_strided(cand, gate, "cand"), *_strided(h, gate, "h"), *r,
+            _like(h0, dev, states, torch.float32, "h0"), _like(lengths, dev, shape[1:2], torch.int32, "lengths"))
 
 
-def _scan_ws(T, Bn, H, ws, dev):
-    n = lib.gated_scan_workspace_bytes(T, Bn, H)
+def _scan_ws(shape, ws, dev):
+    n = lib.gated_scan_workspace_bytes(*shape)
     if n == 0:
         return None, 0
     if ws is None or ws.numel() < n:
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
-    _require(ws.device == dev and ws.dtype == torch.uint8 and ws.is_contiguous(), f"ws: contiguous uint8 array on {dev} required")
+    _require(ws.device == dev and ws.dtype == torch.uint8 and ws.is_contiguous(), "ws: contiguous uint8 array on {} required", dev)
     return ws.data_ptr(), ws.numel()
 
 
@@ -440,14 +450,15 @@ def gated_scan_forward(gate, cand, h0=None, cell=CELL_IMPLICIT, dt=1.0, lengths=
     cell: CELL_CLASSIC, CELL_IMPLICIT (a, b from sigmoid(gate) and tanh(cand)) or SCAN_COEFFICIENTS (a = gate, b = cand).
     h0[B,H] fp32; lengths[B] int32; reset[T,B] uint8 or bool: the sequence starts anew there.  hT may be h0: one call with T = 1 is a step
     of generation that updates the state in place.  Behind a sequence's end h is zero and hT keeps the state."""
-    dev = gate.device
-    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
-    T, Bn, H = gate.shape
-    h = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if h is None else h
-    hT = torch.empty(Bn, H, device=dev) if hT is None else hT
-    args = _scan_args(gate, cand, h, reset, lengths, h0, cell, dt)
-    packed = _SCAN_ARGS.pack(*args, _like(hT, dev, (Bn, H), torch.float32, "hT"), *(0,) * 11)
-    _on_device(dev, lib.gated_scan_forward, packed, *_scan_ws(T, Bn, H, ws, dev))
+    shape, dev = _scan_sizes(gate), gate.device
+    states = shape[1:]
+    if h is None:
+        h = gate.new_empty(shape)
+    if hT is None:
+        hT = gate.new_empty(states, dtype=torch.float32)
+    packed = _SCAN_ARGS.pack(*_scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev), _like(hT, dev, states, torch.float32, "hT"),
+                             0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    _run(dev, lib.gated_scan_forward, packed, *_scan_ws(shape, ws, dev))
     return h, hT
 
 
@@ -455,16 +466,15 @@ def gated_scan_backward(gate, cand, h, h0=None, dh_seed=None, dhT=None, cell=CEL
                         dcand=None, dh0=None, ws=None):
     """Gradients of gated_scan_forward at its states h, given dh_seed[T,B,H] (w.r.t. every h_t) and / or dhT[B,H] (w.r.t. hT)
     -> (dgate, dcand, dh0[B,H] fp32)."""
-    dev = gate.device
-    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
-    T, Bn, H = gate.shape
-    dgate = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if dgate is None else dgate
-    dcand = torch.empty(T, Bn, H, dtype=gate.dtype, device=dev) if dcand is None else dcand
-    dh0 = torch.empty(Bn, H, device=dev) if dh0 is None else dh0
-    args = _scan_args(gate, cand, h, reset, lengths, h0, cell, dt)
-    packed = _SCAN_ARGS.pack(*args, 0, *_strided(dh_seed, gate, "dh_seed"), _like(dhT, dev, (Bn, H), torch.float32, "dhT"), *_strided(dgate, gate, "dgate"),
-                             *_strided(dcand, gate, "dcand"), _like(dh0, dev, (Bn, H), torch.float32, "dh0"))
-    _on_device(dev, lib.gated_scan_backward, packed, *_scan_ws(T, Bn, H, ws, dev))
+    shape, dev = _scan_sizes(gate), gate.device
+    states = shape[1:]
+    dgate = gate.new_empty(shape) if dgate is None else dgate
+    dcand = gate.new_empty(shape) if dcand is None else dcand
+    dh0 = gate.new_empty(states, dtype=torch.float32) if dh0 is None else dh0
+    packed = _SCAN_ARGS.pack(*_scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev), 0, *_strided(dh_seed, gate, "dh_seed"),
+                             _like(dhT, dev, states, torch.float32, "dhT"), *_strided(dgate, gate, "dgate"), *_strided(dcand, gate, "dcand"),
+                             _like(dh0, dev, states, torch.float32, "dh0"))
+    _run(dev, lib.gated_scan_backward, packed, *_scan_ws(shape, ws, dev))
     return dgate, dcand, dh0
 
 
@@ -479,10 +489,11 @@ class TokenLogprobs:
 
 def _logit_rows(t, name, like=None):
     """(address, elements from row to row) of a matrix of logits with contiguous rows."""
-    _require(t.dim() == 2 and t.is_cuda and (like is None or (t.shape == like.shape and t.dtype == like.dtype and t.device == like.device)),
-             f"{name}: CUDA matrix [N,V] required" + ("" if like is None else ", of the logits' shape, type and device"))
-    _require(t.stride(1) == 1 or t.shape[1] == 1, f"{name}: the elements of a row must be contiguous")
-    return t.data_ptr(), t.stride(0)
+    if t.dim() != 2 or not t.is_cuda or (like is not None and not (t.shape == like.shape and t.dtype is like.dtype and t.device == like.device)):
+        raise ValueError(f"{name}: CUDA matrix [N,V] required" + ("" if like is None else ", of the logits' shape, type and device"))
+    ld, one = t.stride()
+    _require(one == 1 or t.shape[1] == 1, "{}: the elements of a row must be contiguous", name)
+    return t.data_ptr(), ld
 
 
 def token_logprobs(logits, tokens=None, top=0, out=None):
@@ -491,12 +502,14 @@ def token_logprobs(logits, tokens=None, top=0, out=None):
     -> TokenLogprobs of fp32 arrays (top_id int32).  `out`: a TokenLogprobs of an earlier call of the same sizes, to be overwritten."""
     p, ld = _logit_rows(logits, "logits")
     (N, V), dev, f32 = logits.shape, logits.device, torch.float32
+    rows = logits.shape[:1]
     if out is None:
-        out = TokenLogprobs(None if tokens is None else torch.empty(N, device=dev), torch.empty(N, device=dev), torch.empty(N, device=dev),
-                            torch.empty(N, top, device=dev) if top > 0 else None, torch.empty(N, top, dtype=torch.int32, device=dev) if top > 0 else None)
-    _on_device(dev, lib.token_logprobs, N, V, _dtype(logits), p, ld, _like(tokens, dev, (N,), torch.int32, "tokens"), top,
-               _like(out.logprob, dev, (N,), f32, "logprob"), _like(out.entropy, dev, (N,), f32, "entropy"), _like(out.lse, dev, (N,), f32, "lse"),
-               _like(out.top_logprob, dev, (N, top), f32, "top_logprob"), _like(out.top_id, dev, (N, top), torch.int32, "top_id"))
+        each, ent, lse = logits.new_empty((3, N), dtype=f32).unbind()
+        out = TokenLogprobs(None if tokens is None else each, ent, lse, logits.new_empty((N, top), dtype=f32) if top > 0 else None,
+                            logits.new_empty((N, top), dtype=torch.int32) if top > 0 else None)
+    _run(dev, lib.token_logprobs, N, V, _dtype(logits), p, ld, _like(tokens, dev, rows, torch.int32, "tokens"), top,
+         _like(out.logprob, dev, rows, f32, "logprob"), _like(out.entropy, dev, rows, f32, "entropy"), _like(out.lse, dev, rows, f32, "lse"),
+         _like(out.top_logprob, dev, (N, top), f32, "top_logprob"), _like(out.top_id, dev, (N, top), torch.int32, "top_id"))
     return out
 
 
@@ -505,11 +518,12 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogprob=None, de
     forward call returned.  dlogits may be the logits themselves (in place).  -> dlogits[N,V]"""
     p, ld = _logit_rows(logits, "logits")
     (N, V), dev, f32 = logits.shape, logits.device, torch.float32
-    dlogits = torch.empty(N, V, dtype=logits.dtype, device=dev) if dlogits is None else dlogits
+    rows = logits.shape[:1]
+    dlogits = logits.new_empty((N, V)) if dlogits is None else dlogits
     d, dld = _logit_rows(dlogits, "dlogits", logits)
-    _on_device(dev, lib.token_logprobs_backward, N, V, _dtype(logits), p, ld, _like(tokens, dev, (N,), torch.int32, "tokens") if dlogprob is not None else 0,
-               _like(lse, dev, (N,), f32, "lse"), _like(entropy, dev, (N,), f32, "entropy") if dentropy is not None else 0,
-               _like(dlogprob, dev, (N,), f32, "dlogprob"), _like(dentropy, dev, (N,), f32, "dentropy"), d, dld)
+    _run(dev, lib.token_logprobs_backward, N, V, _dtype(logits), p, ld, _like(tokens, dev, rows, torch.int32, "tokens") if dlogprob is not None else 0,
+         _like(lse, dev, rows, f32, "lse"), _like(entropy, dev, rows, f32, "entropy") if dentropy is not None else 0,
+         _like(dlogprob, dev, rows, f32, "dlogprob"), _like(dentropy, dev, rows, f32, "dentropy"), d, dld)
     return dlogits
 
 
@@ -520,13 +534,14 @@ def distill_topk_fwd_bwd(logits, top_id, top_logit, weight=None, temperature=1.0
     p, ld = _logit_rows(logits, "logits")
     _require(top_id.dim() == 2, "top_id: matrix [N,K] required")
     (N, V), K, dev, f32 = logits.shape, top_id.shape[1], logits.device, torch.float32
-    dlogits = torch.empty(N, V, dtype=logits.dtype, device=dev) if dlogits is None else dlogits
+    rows = logits.shape[:1]
+    dlogits = logits.new_empty((N, V)) if dlogits is None else dlogits
+    loss = logits.new_empty(1, dtype=f32) if loss is None else loss
+    row_loss = logits.new_empty(rows, dtype=f32) if row_loss is None else row_loss
     d, dld = _logit_rows(dlogits, "dlogits", logits)
-    loss = torch.empty(1, device=dev) if loss is None else loss
-    row_loss = torch.empty(N, device=dev) if row_loss is None else row_loss
-    _on_device(dev, lib.distill_topk_fwd_bwd, N, V, K, _dtype(logits), temperature, p, ld, _like(top_id, dev, (N, K), torch.int32, "top_id"),
-               _like(top_logit, dev, (N, K), f32, "top_logit"), _like(weight, dev, (N,), f32, "weight"), _like(loss, dev, (1,), f32, "loss"),
-               _like(row_loss, dev, (N,), f32, "row_loss"), d, dld)
+    _run(dev, lib.distill_topk_fwd_bwd, N, V, K, _dtype(logits), temperature, p, ld, _like(top_id, dev, (N, K), torch.int32, "top_id"),
+         _like(top_logit, dev, (N, K), f32, "top_logit"), _like(weight, dev, rows, f32, "weight"), _like(loss, dev, (1,), f32, "loss"),
+         _like(row_loss, dev, rows, f32, "row_loss"), d, dld)
     return loss, row_loss, dlogits
 
 

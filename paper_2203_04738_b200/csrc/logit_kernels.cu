@@ -4,7 +4,7 @@
 // All are bound by HBM (a row is read once, gradients are written once) with one or two exponentials an element, which take up to three
 // quarters of that time (16 a cycle and SM).
 //  * short rows (V <= 1024): a group of 8 or 32 lanes has a row, in registers;
-//  * longer ones: a block, or a cluster of up to 16 that meet through distributed shared memory, one for about 64 KB of a row.  The first
+//  * longer ones: a block, or a cluster of up to 16 that meet through distributed shared memory.  The first
 //    pass streams the row once with a reference for the exponents that only moves when it has to; what is looked at twice (the gradient's
 //    pass, the vectors that hold a top alternative) comes from L2, where the rows in work have room.  Small blocks and no state but the
 //    sums: holding a row in registers or shared memory instead took 138 us for distillation of 4096 x 32768 in bf16 (bytes: 82), bound
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kMaxTop = 128, kMaxTeacher = 1024;
 constexpr int kRow = 256, kBatch = 4;          // threads of a block, 16-byte vectors of a thread at a time
+constexpr int kBlocks = 5;                     // on an SM: registers are kept to that (4: 115 us for distillation of 4096 x 32768 bf16; 5: 110)
 constexpr int kMaxCluster = 16;
 constexpr int kShortRow = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -208,7 +209,7 @@ template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsig
 // their logits again, as a rule at one batch of them, since a thread knows the largest logit of its best batch and of all the others.  What
 // they find, little more than `top`, is put in order by counting.  Where ties or a NaN make it much, the largest is taken out `top` times.
 template <class T, bool TOP>
-__global__ void __launch_bounds__(kRow, 4) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
+__global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restrict__ logits, const LogprobArgs a, int cluster) {
   constexpr int E = V16<T>::E, NW = kRow / 32;
   __shared__ unsigned long long list[TOP ? kList : 1];
   __shared__ unsigned long long best[TOP ? kMaxTop : 1];
@@ -372,14 +373,27 @@ __global__ void __launch_bounds__(kRow, 4) logprob_kernel(const T* __restrict__ 
     all = Stats{__shfl_sync(0xffffffffu, all.m, 0), __shfl_sync(0xffffffffu, all.s, 0), __shfl_sync(0xffffffffu, all.w, 0)};
     if (threadIdx.x == 0) write_row(a, row, r, all);
     if (TOP) {
-      const int total = cluster * a.top;       // (places without an alternative hold zero, below every key)
-      for (int k = threadIdx.x; k < total; k += kRow) {
+      // each block's own are in order: at least `top` of all reach the lowest of the blocks' j-th ones
+      const int j = (a.top + cluster - 1) / cluster;
+      unsigned long long least = ~0ull;
+      if (lane < cluster) least = j <= elements_of(row, a.V, cluster, lane) ? blocks.map_shared_rank(best, lane)[j - 1] : 0ull;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long other = __shfl_xor_sync(0xffffffffu, least, o);
+        least = other < least ? other : least;
+      }
+      if (threadIdx.x == 0) count = 0;
+      __syncthreads();
+      for (int k = threadIdx.x; k < cluster * a.top; k += kRow) {
         const int c = k / a.top;
-        list[k] = k - c * a.top < elements_of(row, a.V, cluster, c) ? blocks.map_shared_rank(best, c)[k - c * a.top] : 0ull;
+        if (k - c * a.top < elements_of(row, a.V, cluster, c)) {
+          const unsigned long long key = blocks.map_shared_rank(best, c)[k - c * a.top];
+          if (key >= least) list[atomicAdd(&count, 1)] = key;
+        }
       }
       __syncthreads();
       const float ls = log_sum(all);
-      by_rank<kRow>(list, total, a.top, [&](int k, unsigned long long key) { answer(k, key, all, ls); });
+      by_rank<kRow>(list, count, a.top, [&](int k, unsigned long long key) { answer(k, key, all, ls); });
     }
   }
   blocks.sync();                               // nobody leaves while its shared memory may be read
@@ -429,25 +443,26 @@ __global__ void __launch_bounds__(kShortThreads) logprob_short_kernel(const T* _
   if (m == -INFINITY) t.s = t.w = 0.f;
   if (l == 0 && live) write_row(a, row, r, t);
   if (a.top == 0) return;
-  // the largest key, `top` times; a lane knows the largest of its own and looks for the next one when it is taken
+  // the largest one, `top` times: its value's key (0: taken, or no logit), then the lowest token that has it
   const float ls = log_sum(t);
-  unsigned long long last = ~0ull;
+  unsigned key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) key[i] = i * G + l < a.V ? value_key(x[i]) + 1u : 0u;
   for (int k = 0; k < a.top; ++k) {
-    unsigned long long high = 0;
+    unsigned high = 0u, v = 0xffffffffu;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const unsigned long long key = top_key(x[i], i * G + l);
-      if (i * G + l < a.V && key < last && key > high) high = key;
-    }
+    for (int i = 0; i < PER; ++i) high = max(high, key[i]);
 #pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) {
-      const unsigned long long other = __shfl_xor_sync(0xffffffffu, high, o, G);
-      high = other > high ? other : high;
-    }
-    last = high;
+    for (int o = G / 2; o > 0; o >>= 1) high = max(high, __shfl_xor_sync(0xffffffffu, high, o, G));
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) v = key[i] == high ? (unsigned)(i * G + l) : v;
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = min(v, __shfl_xor_sync(0xffffffffu, v, o, G));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = v == (unsigned)(i * G + l) ? 0u : key[i];
     if (l == 0 && live) {
-      a.top_id[(i64)r * a.top + k] = key_token(last);
-      a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value((unsigned)(last >> 32)), t, ls);
+      a.top_id[(i64)r * a.top + k] = (int)v;
+      a.top_logprob[(i64)r * a.top + k] = logprob_of(key_value(high - 1u), t, ls);
     }
   }
 }
@@ -525,7 +540,7 @@ struct Student { float m, s; };
 // Two passes over a row, the second from L2.  The gradient of the whole row is scale q; the places of the teacher's alternatives are written
 // once more, by the first of those that name the same token, after the block has written the rest.
 template <class T>
-__global__ void __launch_bounds__(kRow, 4) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
+__global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
   constexpr int E = V16<T>::E, NW = kRow / 32;
   extern __shared__ float teacher[];           // [K] logit / tau, then probability; [K] the student's logit; [K] token
   float *prob = teacher, *gap = prob + a.K;
@@ -795,11 +810,12 @@ int launched(cudaError_t e) {
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
-// Blocks that share a row: one for about 64 KB of it; more of them, down to 8 KB each, where that leaves SMs without work.
-int blocks_of(int N, i64 bytes) {
+// Blocks that share a row: more than one where rows alone leave SMs without work, down to 8 KB each, and for a row that is read twice, one for
+// each 128 KB of it, so that the rows in work stay in L2.
+int blocks_of(int N, i64 bytes, bool twice) {
   int c = 1;
-  while (c < kMaxCluster && bytes > c * (i64)65536) c *= 2;
-  while (c < kMaxCluster && (i64)N * c < 148 && bytes >= 2 * c * (i64)8192) c *= 2;
+  while (twice && c < kMaxCluster && bytes > c * (i64)131072) c *= 2;
+  while (c < kMaxCluster && (i64)N * c < 296 && bytes >= 2 * c * (i64)8192) c *= 2;
   return c;
 }
 template <class... KArgs, class... Args>
@@ -831,7 +847,7 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
     using T = decltype(tag);
     const T* x = static_cast<const T*>(logits);
     cudaStream_t s = (cudaStream_t)stream;
-    const int c = blocks_of(N, (i64)V * (i64)sizeof(T));
+    const int c = blocks_of(N, (i64)V * (i64)sizeof(T), false);
     const auto few = [&](auto kern, int lanes) { e = launch_pdl(kern, dim3((unsigned)(((i64)N * lanes + kShortThreads - 1) / kShortThreads)), dim3(kShortThreads), 0, s, x, a); };
     if (V <= 64) few(logprob_short_kernel<T, 8, 8>, 8);
     else if (V <= 256) few(logprob_short_kernel<T, 32, 8>, 32);
@@ -885,7 +901,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
       using T = decltype(tag);
       const T* x = static_cast<const T*>(logits);
       T* d = static_cast<T*>(dlogits);
-      const int c = blocks_of(N, (i64)V * (i64)sizeof(T));
+      const int c = blocks_of(N, (i64)V * (i64)sizeof(T), true);
       const auto few = [&](auto kern, int lanes) {
         const i64 blocks = ((i64)N * lanes + kShortThreads - 1) / kShortThreads;
         added = blocks == 1;

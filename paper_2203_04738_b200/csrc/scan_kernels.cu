@@ -714,6 +714,11 @@ ScanSpace scan_space(i64 nk, i64 padded) {
   return s;
 }
 
+size_t scan_workspace(int T, int B, int H) {
+  if (!scan_sizes_served(T, B, H) || T <= kLeastSteps || B == 0) return 0;
+  return scan_space(((i64)T + kLeastSteps - 1) / kLeastSteps, ((i64)B * ((H + 3) / 4 * 4) + kWidest - 1) / kWidest * kWidest).total;
+}
+
 int* scan_status_ptr() {
   const int dev = current_device_slot();
   if (dev < 0) return nullptr;
@@ -747,7 +752,7 @@ template <class K> int resident_blocks(K kern, int threads, int smem, int (&know
   return known[dev];
 }
 
-template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs& a, void* ws, size_t ws_bytes, cudaStream_t s) {
+template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs& a, void* ws, cudaStream_t s) {
   constexpr int VC = kWide<T>;
   if (a.T <= kShort) {
     constexpr int VS = ALIGNED ? VC : 1;
@@ -763,8 +768,6 @@ template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs
     a.nk = (int)nk; a.nc = (int)nc;
     if (nk > 1) {
       const ScanSpace sp = scan_space(nk, nc * wide);
-      if (!ws || ((uintptr_t)ws & 255u)) return MGRIT_INVALID_ARG;
-      if (ws_bytes < sp.total) return MGRIT_WORKSPACE_TOO_SMALL;
       char* w = static_cast<char*>(ws);
       a.ticket = reinterpret_cast<unsigned*>(w);
       a.states = reinterpret_cast<float*>(w + sp.states);
@@ -789,13 +792,16 @@ int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cud
   int rc = check_scan(x, back, a);
   if (rc != MGRIT_OK) return rc;
   if (a.T == 0 || a.B == 0) return back ? copy_state(a.dh0, a.dhT, (size_t)a.B * a.H, s) : copy_state(a.hT, a.h0, (size_t)a.B * a.H, s);
+  const size_t need = scan_workspace(a.T, a.B, a.H);
+  if (need > 0 && (!ws || ((uintptr_t)ws & 255u))) return MGRIT_INVALID_ARG;
+  if (ws_bytes < need) return MGRIT_WORKSPACE_TOO_SMALL;
   const bool wide = wide_columns(a, x->dtype), given = x->cell == MGRIT_SCAN_COEFFICIENTS;
   with_elem(x->dtype, [&](auto tag) {
     using T = decltype(tag);
     const auto pick = [&](auto g) {
       constexpr bool G = decltype(g)::value;
-      rc = wide ? (back ? launch_scan<T, G, true, true>(a, ws, ws_bytes, s) : launch_scan<T, G, true, false>(a, ws, ws_bytes, s))
-               : (back ? launch_scan<T, G, false, true>(a, ws, ws_bytes, s) : launch_scan<T, G, false, false>(a, ws, ws_bytes, s));
+      rc = wide ? (back ? launch_scan<T, G, true, true>(a, ws, s) : launch_scan<T, G, true, false>(a, ws, s))
+               : (back ? launch_scan<T, G, false, true>(a, ws, s) : launch_scan<T, G, false, false>(a, ws, s));
     };
     if (given) pick(std::true_type{}); else pick(std::false_type{});
   });
@@ -822,10 +828,7 @@ int scan_clear_device_status() {
 
 extern "C" {
 
-size_t gated_scan_workspace_bytes(int32_t T, int32_t B, int32_t H) {
-  if (!mg::scan_sizes_served(T, B, H) || T <= mg::kLeastSteps || B == 0) return 0;
-  return mg::scan_space(((mg::i64)T + mg::kLeastSteps - 1) / mg::kLeastSteps, ((mg::i64)B * ((H + 3) / 4 * 4) + mg::kWidest - 1) / mg::kWidest * mg::kWidest).total;
-}
+size_t gated_scan_workspace_bytes(int32_t T, int32_t B, int32_t H) { return mg::scan_workspace(T, B, H); }
 
 int gated_scan_forward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream) {
   return mg::run_scan(args, false, ws, ws_bytes, (cudaStream_t)stream);
