@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -11,7 +13,7 @@ LIB = os.path.join(HERE, "libmgrit_gru.so")
 SOURCES = ["api.cu", "simt_kernels.cu", "f32_solve.cu", "stream_kernels.cu", "umma_engine.cu", "serial_kernels.cu", "scan_kernels.cu",
            "logit_kernels.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-         "-Xcompiler", "-fPIC", "-shared"]
+         "-Xcompiler", "-fPIC"]
 
 
 def _stale() -> bool:
@@ -27,11 +29,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     extra = os.environ.get("MGRIT_GRU_NVCC_FLAGS", "").split()      # e.g. -D switches of kernel variants under study
-    cmd = [nvcc] + FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or r.returncode != 0:
-        sys.stderr.write(r.stdout + r.stderr)
-    if r.returncode != 0:
+    with tempfile.TemporaryDirectory() as tmp:                      # every source by itself, all at once, then one link
+        objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        cmds = [[nvcc] + FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objs)]
+        with ThreadPoolExecutor(min(len(cmds), os.cpu_count() or 1)) as pool:
+            runs = list(pool.map(lambda c: subprocess.run(c, capture_output=True, text=True), cmds))
+        if all(r.returncode == 0 for r in runs):
+            runs.append(subprocess.run([nvcc] + FLAGS + extra + ["-shared", "-o", LIB] + objs, capture_output=True, text=True))
+    failed = any(r.returncode != 0 for r in runs)
+    if verbose or failed:
+        sys.stderr.write("".join(r.stdout + r.stderr for r in runs))
+    if failed:
         raise RuntimeError("nvcc failed building libmgrit_gru.so")
     return LIB
 

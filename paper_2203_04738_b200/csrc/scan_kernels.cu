@@ -17,6 +17,11 @@
 //    differs from it is there.  So publishing is a plain store and looking one trip to L2, without fences.
 //
 // Backward is the same scan from the last step to the first: mu_t = a_t (seed_t + mu_{t+1}).
+//
+// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 116 (61), backward 196 (123);
+// 65536 steps of 1024 units in fp32 forward 257 (123); one step of 32 x 1024 4.4.  What bounds it: two warps on each scheduler that issue
+// dependent arithmetic (42 % of the issue slots, exponentials and reciprocals 40 % of theirs, DRAM 39 %); with given coefficients the first
+// takes 80.  Few columns: the chain of tiles, 0.13 us each at 512 tiles.
 #include <type_traits>
 
 #include "elem.cuh"
@@ -41,47 +46,22 @@ struct ScanArgs {
 
 constexpr int kShort = 8;                      // steps that one thread walks
 constexpr int kShortThreads = 128;
-#ifndef SCAN_W
-#define SCAN_W 8
-#endif
-#ifndef SCAN_SF
-#define SCAN_SF 16
-#endif
-#ifndef SCAN_SB
-#define SCAN_SB 8
-#endif
-#ifndef SCAN_BF
-#define SCAN_BF 1
-#endif
-#ifndef SCAN_BB
-#define SCAN_BB 1
-#endif
-#ifndef SCAN_U
-#define SCAN_U 8
-#endif
-#ifndef SCAN_UB
-#define SCAN_UB 4
-#endif
-#ifndef SCAN_BU
-#define SCAN_BU 1
-#endif
-constexpr int kWarps = SCAN_W;
-template <class T> constexpr int kWide = 8 / sizeof(T);      // columns of a thread: 8 bytes of a row
-// Steps of a thread, and blocks on an SM that registers are kept free for.  ALIGNED rows are staged in shared memory, others in registers.
-template <bool ALIGNED, bool BACK> constexpr int kStepsOf = ALIGNED ? (BACK ? SCAN_SB : SCAN_SF) : BACK ? SCAN_UB : SCAN_U;
-template <bool ALIGNED, bool BACK> constexpr int kBlocksOf = ALIGNED ? (BACK ? SCAN_BB : SCAN_BF) : SCAN_BU;
-#ifndef SCAN_D
-#define SCAN_D 1
-#endif
-constexpr int kAhead = SCAN_D;                 // tiles whose loads are in flight behind the one in work
+constexpr int kWarps = 8;
+template <class T> constexpr int kWide = 8 / sizeof(T);      // VC, columns of a thread: 8 bytes of a row
+// S, steps of a thread.  ALIGNED rows are staged in shared memory, others in registers.  Long pieces pay: what a tile costs whatever its
+// size (its place, the pairs of the other warps, one meeting, one look at L2) is shared by 64 elements of a thread, and the chain of tiles is
+// short.  One block fills an SM's registers.  Half the steps and two blocks: 116 -> 134 us forward, 196 -> 243 backward for T 2048, B 32,
+// H 1024 in bf16, 257 -> 323 for 65536 steps of 1024 units in fp32.
+template <bool ALIGNED, bool BACK> constexpr int kStepsOf = (ALIGNED ? 16 : 8) / (BACK ? 2 : 1);
+constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2: 122 us for the 116 above)
 constexpr int kLook = 4;                       // looks of 32 tiles back
-constexpr int kPairs = 2;                      // pairs of a column in flight in a look-back
+constexpr int kFirst = 2, kMore = 16;          // pairs in flight in a look-back: of a column at first, of the thread's columns then
+constexpr int kNarrow = 8;                     // column tiles up to which one warp looks back for its block
 constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
 constexpr float kMaxDt = 1e18f;
 
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp_exact(float x) { const float y = rcp(x); return fmaf(fmaf(-x, y, 1.0f), y, y); }      // one Newton step
-
 
 // VC consecutive elements of a row, moved as one word
 template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
@@ -275,7 +255,7 @@ __device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, uns
 // The state in front of tile k of column tile c, for the warp's columns: carried from the last published state through the pairs after
 // it.  Words of a tile are published together, so one of them (the first column's) tells the lanes how far back to go.  A tile that found
 // the state in front of it at once publishes no pair, only its state: whoever misses a word looks again from the start.
-template <int VC> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, i64 row, i64 col, int lane) {
+template <int VC, bool NARROW> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, i64 row, i64 col, int lane) {
   uint64_t t0 = 0;
   for (unsigned round = 0; !waited_too_long(a, lane, round, t0); ++round) {
     int from = -1;                             // the tile whose state is taken
@@ -295,24 +275,34 @@ template <int VC> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, 
       there = there && w != kNone;
       h.at(v) = __uint_as_float(w);
     }
-#pragma unroll 1
-    for (int j = from + 1; j < k && there; j += kPairs) {
-      float2 p[kPairs][VC];
-      const int n = min(kPairs, k - j);
+    // the pairs after it: two at first, which often are not there yet; NARROW: then many in one trip
+    const auto carry = [&](int j, auto pairs) {
+      constexpr int P = decltype(pairs)::value;
+      float2 p[P][VC];
+      const int n = min(P, k - j);
       const unsigned long long* at = a.pairs + j * row + col + lane * VC;
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i)
+      for (int i = 0; i < P; ++i)
 #pragma unroll
         for (int v = 0; v < VC; ++v) p[i][v] = i < n ? ld_pair(at + i * row + v) : make_float2(1.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i)
+      for (int i = 0; i < P; ++i)
 #pragma unroll
         for (int v = 0; v < VC; ++v)
           if (i < n) {
             there = there && __float_as_uint(p[i][v].x) != kNone;
             h.at(v) = through(p[i][v], h.at(v), a.reset.p != nullptr);
           }
+      return j + P;
+    };
+    int j = from + 1;
+    if (NARROW && j + kFirst < k) {
+      j = carry(j, std::integral_constant<int, kFirst>{});
+#pragma unroll 1
+      while (j + kFirst < k && there) j = carry(j, std::integral_constant<int, kMore / VC>{});
     }
+#pragma unroll 1
+    while (j < k && there) j = carry(j, std::integral_constant<int, kFirst>{});
     if (__all_sync(0xffffffffu, there)) return h;
   }
   return F<VC>::all(__uint_as_float(0x7fc00000u));      // the results are void, and look it
@@ -331,8 +321,8 @@ __device__ __forceinline__ Place place_of(const ScanArgs& a, unsigned tile, int 
   return p;
 }
 
-template <class T, bool GIVEN, bool STAGED, bool BACK>
-__global__ void __launch_bounds__(kWarps * 32, kBlocksOf<STAGED, BACK>) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
+template <class T, bool GIVEN, bool STAGED, bool BACK, bool NARROW>
+__global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
   constexpr int VC = kWide<T>, S = kStepsOf<STAGED, BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
   extern __shared__ __align__(16) char stage[];      // [tiles ahead][ARRAYS][S][threads] words of 8 bytes
   constexpr unsigned ALL = (1u << S) - 1u;
@@ -341,6 +331,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<STAGED, BACK>) scan_til
   constexpr int D = STAGED ? kAhead : 1, RING = 4;
   static_assert(D < RING - 1, "a place is written while the one before it and those ahead are in use");
   __shared__ Place place[RING];
+  __shared__ V front[NARROW ? 2 : 1][32];      // NARROW: the state in front of the tile
+  __shared__ volatile unsigned posted[2];      // ... and the turn whose state that is
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const i64 row = (i64)a.nc * CT;
   const bool cut = a.reset.p != nullptr;
@@ -451,6 +443,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<STAGED, BACK>) scan_til
     return inside | fresh << 16;
   };
 
+  if (NARROW && threadIdx.x < 2) posted[threadIdx.x] = 0u;      // (turns are counted from 1 there)
   // Tiles are drawn from the counter (which starts at 2^32 - 1) by thread 32.  deep: D + 1 at the start, and from then on one round
   // before a number is told to the others, so that nobody waits for it.  Otherwise (few tiles: they would all go to the first blocks)
   // one at a time, and nothing is fetched ahead.
@@ -569,7 +562,22 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksOf<STAGED, BACK>) scan_til
 #pragma unroll
           for (int v = 0; v < VC; ++v) st_pair(a.pairs + word + v, whole[v]);
         }
-        h = look_back<VC>(a, k, row, (i64)c * CT, lane);
+        if (!NARROW || warp == kWarps - 1) {
+          h = look_back<VC, NARROW>(a, k, row, (i64)c * CT, lane);
+        } else {                               // the last warp asks L2 for all of them
+          uint64_t t0 = 0;
+          for (unsigned round = 0; posted[buf] != turn + 1u; ++round)
+            if ((round & 4095u) == 4095u && waited_too_long(a, lane, 31u, t0)) break;
+          __syncwarp();
+          __threadfence_block();
+          h = front[buf][lane];
+        }
+      }
+      if (NARROW && warp == kWarps - 1) {       // (whether it had to look back or not: the others asked a moment earlier)
+        front[buf][lane] = h;
+        __syncwarp();
+        __threadfence_block();
+        if (lane == 0) posted[buf] = turn + 1u;
       }
     }
     if (speaker) {
@@ -775,13 +783,20 @@ template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs
       a.status = scan_status_ptr();
       if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
     }
-    static int known[kMaxDevices];
+    // Few column tiles: every tile looks far back, and the blocks' warps in each other's way.  One warp then asks for all of them, for many
+    // pairs at a time (16384 steps of 2 x 64 units in bf16: 43 us against 62; 20000 of 1001: 133 against 151).  With more column tiles a
+    // state is usually there, and warps that look for themselves are ahead (4096 steps of 8 x 1024: 78 us against 92).
     constexpr int smem = ALIGNED ? kAhead * (BACK ? 4 : 2) * kStepsOf<ALIGNED, BACK> * kWarps * 32 * 8 : 0;
-    const int most = resident_blocks(scan_tile_kernel<T, GIVEN, ALIGNED, BACK>, kWarps * 32, smem, known);
-    if (most <= 0) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
-    // every block gets four tiles or more: enough that the first ones to run may take several at once
-    a.deep = nk * nc >= 4 * (i64)most;
-    scan_tile_kernel<T, GIVEN, ALIGNED, BACK><<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
+    const auto run = [&](auto kern, int (&known)[kMaxDevices]) {
+      const int most = resident_blocks(kern, kWarps * 32, smem, known);
+      if (most <= 0) { cudaGetLastError(); return false; }
+      // every block gets four tiles or more: enough that the first ones to run may take several at once
+      a.deep = nk * nc >= 4 * (i64)most;
+      kern<<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
+      return true;
+    };
+    static int known[2][kMaxDevices];
+    if (!(nc <= kNarrow ? run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, true>, known[0]) : run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, false>, known[1]))) return MGRIT_CUDA_ERROR;
   }
   count_launch();
   return cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
