@@ -261,7 +261,8 @@ int xent_head_fwd_bwd_noalloc(int32_t B, int32_t H, int32_t C, const float* hT, 
  *
  * Element types of the arrays marked `dtype` below.  States, statistics and losses are fp32 whatever the type; results of 16-bit
  * type are rounded once, to nearest.  These calls need no alignment beyond an element's own size, and no array of theirs may
- * overlap an output except where a call says so. */
+ * overlap an output except where a call says so.  Like the others, their first call on a device sets up the kernels that it uses: make it
+ * before a stream capture is started. */
 enum { MGRIT_F32 = 0, MGRIT_BF16 = 1, MGRIT_F16 = 2 };
 /* Value of gated_scan_args.cell besides MGRIT_CELL_CLASSIC and MGRIT_CELL_IMPLICIT: the coefficients themselves are given. */
 enum { MGRIT_SCAN_COEFFICIENTS = 2 };
@@ -309,7 +310,7 @@ int gated_scan_forward(const gated_scan_args* args, void* ws, size_t ws_bytes, m
 int gated_scan_backward(const gated_scan_args* args, void* ws, size_t ws_bytes, mgrit_stream_t stream);
 
 /* Log probabilities of given tokens, with the entropy of each row's distribution and its `top` most probable tokens.
- *   logits: N rows of V elements (dtype), row r at logits + r * ld (elements; ld >= V, 0 <= top <= min(V, 128)).
+ *   logits: N rows of V elements (dtype), row r at logits + r * ld (elements; ld >= V, N < 2^27, 0 <= top <= min(V, 128)).
  *   tokens[N] (int32) or NULL -> logprob[N] = x[token] - lse, 0 for a token outside [0, V) (a row without a target).
  *   entropy[N] = - sum_v p_v log p_v and lse[N] = log sum_v exp x_v (each may be NULL);
  *   top_logprob[N,top], top_id[N,top] (int32), falling; equal logits in rising order of their token (NULL where top == 0).

@@ -191,6 +191,7 @@ template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& 
 // ---- log probabilities: rows in the registers of a block or a cluster --------------------------------------------------------------
 
 constexpr int kList = 2048;                    // candidates that a block holds: its own, or those of a cluster
+constexpr int kRanked = 512;                   // of its own as many are put in order by counting (2 us); more are ties, and taken out one by one
 static_assert(kList >= kMaxCluster * kMaxTop, "the lists of a whole cluster");
 
 // Writes the `top` largest of n keys, in order, to out(rank, key): each key counts those above it.
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restr
     const auto offer = [&](float x, int v) {
       if (x >= least) {
         const int place = atomicAdd(&count, 1);
-        if (place < kList) list[place] = top_key(x, v);
+        if (place < kRanked) list[place] = top_key(x, v);
       }
     };
     if (p.edge >= 0) offer(edge, p.edge);
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restr
       if (cluster == 1) answer(k, key, all, ls);
       else best[k] = key;
     };
-    if (m == m && found <= kList) {
+    if (m == m && found <= kRanked) {
       by_rank<kRow>(list, found, have, keep);
     } else {
       unsigned long long last = ~0ull;

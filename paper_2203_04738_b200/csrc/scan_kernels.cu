@@ -472,11 +472,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
     const int k = here.k, c = here.c;
     const unsigned buf = turn & 1u;
     const i64 word = k * row + (i64)c * CT + lane * VC;
-    // the state that the tile before has published, asked for early: it is usually there
+    // The state in front: what the tile before has published, asked for early (it is usually there), or the first one, which every warp has
+    // read before the block meets, since the last tile may write its result over it (hT = h0).
     unsigned early[VC];
     if (k > 0) {
 #pragma unroll
       for (int v = 0; v < VC; ++v) early[v] = ld_word(a.states + word - row + v);
+    } else {
+      const V first = load_state<VC>(BACK ? a.dhT : a.h0, now.b * (unsigned)a.H + now.u, now.n);
+#pragma unroll
+      for (int v = 0; v < VC; ++v) early[v] = __float_as_uint(first.at(v));
     }
     const unsigned told = drawn;
     if (threadIdx.x == 32 && a.deep) draw();
@@ -547,16 +552,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
         for (int v = 0; v < VC; ++v) whole[v] = through(pair[buf][w][lane * VC + v], whole[v], cut);
       }
     }
-    if (k == 0) {
-      const float* first = BACK ? a.dhT : a.h0;
-      h = load_state<VC>(first, now.b * (unsigned)a.H + now.u, now.n);
-    } else {
+#pragma unroll
+    for (int v = 0; v < VC; ++v) h.at(v) = __uint_as_float(early[v]);
+    if (k > 0) {
       bool known = true;
 #pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        known = known && early[v] != kNone;
-        h.at(v) = __uint_as_float(early[v]);
-      }
+      for (int v = 0; v < VC; ++v) known = known && early[v] != kNone;
       if (!__all_sync(0xffffffffu, known)) {
         if (speaker) {
 #pragma unroll
@@ -667,7 +668,8 @@ bool rows_apart(const mgrit_rows& r, int T, int B, int H) {
   return (bs >= H && ts / bs >= B - 1 && ts - bs * (B - 1) >= H) || (ts >= H && bs / ts >= T - 1 && bs - ts * (T - 1) >= H);
 }
 
-ScanRows rows_of(const mgrit_rows& r) { return ScanRows{static_cast<char*>(r.data), r.t_stride, r.b_stride}; }
+// (the stride of an axis with one place says nothing)
+ScanRows rows_of(const mgrit_rows& r, const gated_scan_args* x) { return ScanRows{static_cast<char*>(r.data), x->T > 1 ? r.t_stride : 0, x->B > 1 ? r.b_stride : 0}; }
 
 int check_scan(const gated_scan_args* x, bool back, ScanArgs& a) {
   if (!x || x->T < 0 || x->B < 0 || x->H <= 0 || x->cell < 0 || x->cell > MGRIT_SCAN_COEFFICIENTS || !elem_known(x->dtype)) return MGRIT_INVALID_ARG;
@@ -688,11 +690,11 @@ int check_scan(const gated_scan_args* x, bool back, ScanArgs& a) {
   }
   if (x->T == 0 || x->B == 0) return MGRIT_OK;
   if (!x->gate.data || !x->cand.data || !x->h.data) return MGRIT_INVALID_ARG;
-  a.gate = rows_of(x->gate); a.cand = rows_of(x->cand); a.h = rows_of(x->h); a.reset = rows_of(x->reset);
+  a.gate = rows_of(x->gate, x); a.cand = rows_of(x->cand, x); a.h = rows_of(x->h, x); a.reset = rows_of(x->reset, x);
   bool ok = elem_aligned(a.gate.p, x->dtype) && elem_aligned(a.cand.p, x->dtype) && elem_aligned(a.h.p, x->dtype);
   if (back) {
     if (!x->dgate.data || !x->dcand.data || (!x->dh_seed.data && !x->dhT)) return MGRIT_INVALID_ARG;
-    a.seed = rows_of(x->dh_seed); a.dgate = rows_of(x->dgate); a.dcand = rows_of(x->dcand);
+    a.seed = rows_of(x->dh_seed, x); a.dgate = rows_of(x->dgate, x); a.dcand = rows_of(x->dcand, x);
     ok = ok && elem_aligned(a.seed.p, x->dtype) && elem_aligned(a.dgate.p, x->dtype) && elem_aligned(a.dcand.p, x->dtype) &&
          rows_apart(x->dgate, x->T, x->B, x->H) && rows_apart(x->dcand, x->T, x->B, x->H);
   } else {

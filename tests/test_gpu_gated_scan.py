@@ -191,6 +191,46 @@ def test_steps_of_generation_update_the_state_in_place():
     R.check(state, refT, boundT, "chunks")
 
 
+@pytest.mark.parametrize("T,B,H,dtype", [(1, 64, 1024, BF16), (9, 64, 1024, BF16), (60, 64, 1024, F32), (128, 40, 999, F16), (129, 64, 1024, BF16), (700, 16, 512, BF16)])
+def test_the_last_state_may_replace_the_first_one(T, B, H, dtype):
+    """hT = h0 for one tile and several along time: every reader of the first state comes before its writer."""
+    from paper_2203_04738_b200 import binding as L
+    d = make(T, B, H, dtype, R.IMPLICIT, False, False, False, T)
+    want, last = L.gated_scan_forward(d["gate"], d["cand"], h0=d["h0"])
+    for _ in range(30):
+        state = d["h0"].clone()
+        h, hT = L.gated_scan_forward(d["gate"], d["cand"], h0=state, hT=state)
+        assert hT is state and torch.equal(state, last) and torch.equal(h, want)
+
+
+def test_two_calls_at_once_that_fill_the_device():
+    """Each of them wants every SM: blocks of both run side by side, and neither waits for one of its own that has not started."""
+    from paper_2203_04738_b200 import binding as L
+    ds = [make(2500, 8, 1024, BF16, R.IMPLICIT, False, False, s == 2, s) for s in (1, 2)]
+    want = [L.gated_scan_forward(d["gate"], d["cand"], h0=d["h0"]) for d in ds]
+    gwant = [L.gated_scan_backward(d["gate"], d["cand"], w[0], h0=d["h0"], dh_seed=d["seed"]) for d, w in zip(ds, want)]
+    streams = [torch.cuda.Stream() for _ in ds]
+    for _ in range(6):
+        got = []
+        for s, d, w in zip(streams, ds, want):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append([*L.gated_scan_forward(d["gate"], d["cand"], h0=d["h0"]), *L.gated_scan_backward(d["gate"], d["cand"], w[0], h0=d["h0"], dh_seed=d["seed"])])
+        torch.cuda.synchronize()
+        for o, w, g in zip(got, want, gwant):
+            assert all(torch.equal(x, y) for x, y in zip(o, [*w, *g]))
+    assert L.last_device_status() == 0
+
+
+def test_strides_of_single_places_say_nothing():
+    from paper_2203_04738_b200 import binding as L
+    d = make(50, 1, 64, F32, R.IMPLICIT, False, False, False, 4)
+    want, last = L.gated_scan_forward(d["gate"], d["cand"], h0=d["h0"])
+    odd = lambda x: torch.as_strided(x, x.shape, (x.stride(0), 3, 1))
+    h, hT = L.gated_scan_forward(odd(d["gate"].contiguous()), odd(d["cand"].contiguous()), h0=d["h0"])
+    assert torch.equal(h, want) and torch.equal(hT, last)
+
+
 def test_strides_past_32_bits():
     """Rows of a larger array whose offsets in elements pass 2^32: nothing else of the array is touched."""
     from paper_2203_04738_b200 import binding as L

@@ -84,6 +84,18 @@ def test_ties_go_to_the_lower_token(V):
             check_rows(x, [0, 1, 2, V - 1, 4, 5], top, f"{dtype} {top}")
 
 
+@pytest.mark.parametrize("V,equal", [(3000, 400), (3000, 600), (40000, 511), (40000, 520), (131072, 30000)])
+def test_many_equal_best_logits(V, equal):
+    """As many equal candidates as are put in order by counting, and more."""
+    for dtype in (F32, BF16):
+        x = torch.full((3, V), -1.0, dtype=dtype, device="cuda")
+        for r in range(3):
+            x[r, torch.randperm(V, device="cuda")[:equal]] = 4.0
+            x[r, V // 2 + r] = 6.0
+        for top in (1, 20, 128):
+            check_rows(x, [0, V // 2, V - 1], top, f"{dtype} {top}")
+
+
 @pytest.mark.parametrize("V", [40, 1500, 9000, 66000])
 def test_masked_vocabularies_infinities_and_nan(V):
     for dtype in DTYPES:
