@@ -7,6 +7,7 @@ library's kernels -- if the library has not been built, importing this module ra
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import struct
 from dataclasses import dataclass
@@ -406,42 +407,41 @@ def _like(t, dev, shape, dtype, name):
     return t.data_ptr()
 
 
-def _strided(t, like, name):
-    """(address, stride of t, stride of b) of an array of the shape, type and device of `like`."""
+def _strided(t, shape, dtype, dev, name):
+    """(address, stride of t, stride of b) of an array of that shape, type and device with contiguous units."""
     if t is None:
         return 0, 0, 0
-    st, sb, su = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if not (t.shape == like.shape and t.dtype is like.dtype and t.device == like.device and (su == 1 or t.shape[2] == 1)):
-        raise ValueError(f"{name}: {like.dtype} array of shape {tuple(like.shape)} on {like.device} with contiguous units required")
-    return t.data_ptr(), st, sb
+    if t.shape == shape and t.dtype is dtype and t.device == dev:
+        st, sb, su = t.stride()
+        if su == 1 or shape[2] == 1:
+            return t.data_ptr(), st, sb
+    raise ValueError(f"{name}: {dtype} array of shape {tuple(shape)} on {dev} with contiguous units required")
 
 
 _SCAN_ARGS = struct.Struct("@5if" + 3 * "Pqq" + "Pqq" + "PPP" + "Pqq" + "P" + 2 * "Pqq" + "P")      # gated_scan_args
+_scan_ws_bytes = functools.lru_cache(maxsize=4096)(lib.gated_scan_workspace_bytes)      # (of the sizes alone)
 
 
-def _scan_sizes(gate):
-    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
-    return gate.shape
-
-
-def _scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev):
+def _scan_head(gate, cand, h, reset, lengths, h0, cell, dt, shape, dev):
+    """The fields of gated_scan_args that both calls have; h: its (address, strides)."""
+    t = gate.dtype
     if reset is None:
         r = (0, 0, 0)
     else:
         _require(reset.dtype in (torch.uint8, torch.bool) and reset.shape == shape[:2] and reset.device == dev, "reset: uint8 or bool array [T,B] on {} required", dev)
         r = (reset.data_ptr(), *reset.stride())
-    return (*shape, cell, _dtype(gate), dt, *_strided(gate, gate, "gate"), *_strided(cand, gate, "cand"), *_strided(h, gate, "h"), *r,
-            _like(h0, dev, states, torch.float32, "h0"), _like(lengths, dev, shape[1:2], torch.int32, "lengths"))
+    return (*shape, cell, _dtype(gate), dt, *_strided(gate, shape, t, dev, "gate"), *_strided(cand, shape, t, dev, "cand"), *h, *r,
+            0 if h0 is None else _like(h0, dev, shape[1:], torch.float32, "h0"), 0 if lengths is None else _like(lengths, dev, shape[1:2], torch.int32, "lengths"))
 
 
-def _scan_ws(shape, ws, dev):
-    n = lib.gated_scan_workspace_bytes(*shape)
+def _scan_call(fn, packed, shape, ws, dev):
+    n = _scan_ws_bytes(*shape)
     if n == 0:
-        return None, 0
+        return _run(dev, fn, packed, None, 0)
     if ws is None or ws.numel() < n:
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
     _require(ws.device == dev and ws.dtype == torch.uint8 and ws.is_contiguous(), "ws: contiguous uint8 array on {} required", dev)
-    return ws.data_ptr(), ws.numel()
+    _run(dev, fn, packed, ws.data_ptr(), ws.numel())
 
 
 def gated_scan_forward(gate, cand, h0=None, cell=CELL_IMPLICIT, dt=1.0, lengths=None, reset=None, h=None, hT=None, ws=None):
@@ -450,15 +450,20 @@ def gated_scan_forward(gate, cand, h0=None, cell=CELL_IMPLICIT, dt=1.0, lengths=
     cell: CELL_CLASSIC, CELL_IMPLICIT (a, b from sigmoid(gate) and tanh(cand)) or SCAN_COEFFICIENTS (a = gate, b = cand).
     h0[B,H] fp32; lengths[B] int32; reset[T,B] uint8 or bool: the sequence starts anew there.  hT may be h0: one call with T = 1 is a step
     of generation that updates the state in place.  Behind a sequence's end h is zero and hT keeps the state."""
-    shape, dev = _scan_sizes(gate), gate.device
-    states = shape[1:]
+    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
+    shape, dev = gate.shape, gate.device
     if h is None:
         h = gate.new_empty(shape)
+        rows = (h.data_ptr(), shape[1] * shape[2], shape[2])
+    else:
+        rows = _strided(h, shape, gate.dtype, dev, "h")
     if hT is None:
-        hT = gate.new_empty(states, dtype=torch.float32)
-    packed = _SCAN_ARGS.pack(*_scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev), _like(hT, dev, states, torch.float32, "hT"),
-                             0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
-    _run(dev, lib.gated_scan_forward, packed, *_scan_ws(shape, ws, dev))
+        hT = gate.new_empty(shape[1:], dtype=torch.float32)
+        last = hT.data_ptr()
+    else:
+        last = _like(hT, dev, shape[1:], torch.float32, "hT")
+    packed = _SCAN_ARGS.pack(*_scan_head(gate, cand, rows, reset, lengths, h0, cell, dt, shape, dev), last, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    _scan_call(lib.gated_scan_forward, packed, shape, ws, dev)
     return h, hT
 
 
@@ -466,15 +471,15 @@ def gated_scan_backward(gate, cand, h, h0=None, dh_seed=None, dhT=None, cell=CEL
                         dcand=None, dh0=None, ws=None):
     """Gradients of gated_scan_forward at its states h, given dh_seed[T,B,H] (w.r.t. every h_t) and / or dhT[B,H] (w.r.t. hT)
     -> (dgate, dcand, dh0[B,H] fp32)."""
-    shape, dev = _scan_sizes(gate), gate.device
-    states = shape[1:]
+    _require(gate.dim() == 3 and gate.is_cuda, "gate: CUDA array [T,B,H] required")
+    shape, dev, t = gate.shape, gate.device, gate.dtype
     dgate = gate.new_empty(shape) if dgate is None else dgate
     dcand = gate.new_empty(shape) if dcand is None else dcand
-    dh0 = gate.new_empty(states, dtype=torch.float32) if dh0 is None else dh0
-    packed = _SCAN_ARGS.pack(*_scan_args(gate, cand, h, reset, lengths, h0, cell, dt, shape, states, dev), 0, *_strided(dh_seed, gate, "dh_seed"),
-                             _like(dhT, dev, states, torch.float32, "dhT"), *_strided(dgate, gate, "dgate"), *_strided(dcand, gate, "dcand"),
-                             _like(dh0, dev, states, torch.float32, "dh0"))
-    _run(dev, lib.gated_scan_backward, packed, *_scan_ws(shape, ws, dev))
+    dh0 = gate.new_empty(shape[1:], dtype=torch.float32) if dh0 is None else dh0
+    packed = _SCAN_ARGS.pack(*_scan_head(gate, cand, _strided(h, shape, t, dev, "h"), reset, lengths, h0, cell, dt, shape, dev), 0,
+                             *_strided(dh_seed, shape, t, dev, "dh_seed"), _like(dhT, dev, shape[1:], torch.float32, "dhT"),
+                             *_strided(dgate, shape, t, dev, "dgate"), *_strided(dcand, shape, t, dev, "dcand"), _like(dh0, dev, shape[1:], torch.float32, "dh0"))
+    _scan_call(lib.gated_scan_backward, packed, shape, ws, dev)
     return dgate, dcand, dh0
 
 
@@ -501,15 +506,19 @@ def token_logprobs(logits, tokens=None, top=0, out=None):
     exponentials of each row, and its `top` most probable tokens (equal logits: the lower token first; top <= 128)
     -> TokenLogprobs of fp32 arrays (top_id int32).  `out`: a TokenLogprobs of an earlier call of the same sizes, to be overwritten."""
     p, ld = _logit_rows(logits, "logits")
-    (N, V), dev, f32 = logits.shape, logits.device, torch.float32
-    rows = logits.shape[:1]
+    shape, dev, f32 = logits.shape, logits.device, torch.float32
+    N, V = shape
     if out is None:
         each, ent, lse = logits.new_empty((3, N), dtype=f32).unbind()
         out = TokenLogprobs(None if tokens is None else each, ent, lse, logits.new_empty((N, top), dtype=f32) if top > 0 else None,
                             logits.new_empty((N, top), dtype=torch.int32) if top > 0 else None)
-    _run(dev, lib.token_logprobs, N, V, _dtype(logits), p, ld, _like(tokens, dev, rows, torch.int32, "tokens"), top,
-         _like(out.logprob, dev, rows, f32, "logprob"), _like(out.entropy, dev, rows, f32, "entropy"), _like(out.lse, dev, rows, f32, "lse"),
-         _like(out.top_logprob, dev, (N, top), f32, "top_logprob"), _like(out.top_id, dev, (N, top), torch.int32, "top_id"))
+        q = each.data_ptr()
+        to = (q if tokens is not None else 0, q + 4 * N, q + 8 * N, out.top_logprob.data_ptr() if top > 0 else 0, out.top_id.data_ptr() if top > 0 else 0)
+    else:
+        rows = shape[:1]
+        to = (_like(out.logprob, dev, rows, f32, "logprob"), _like(out.entropy, dev, rows, f32, "entropy"), _like(out.lse, dev, rows, f32, "lse"),
+              _like(out.top_logprob, dev, (N, top), f32, "top_logprob"), _like(out.top_id, dev, (N, top), torch.int32, "top_id"))
+    _run(dev, lib.token_logprobs, N, V, _dtype(logits), p, ld, 0 if tokens is None else _like(tokens, dev, shape[:1], torch.int32, "tokens"), top, *to)
     return out
 
 
@@ -535,13 +544,22 @@ def distill_topk_fwd_bwd(logits, top_id, top_logit, weight=None, temperature=1.0
     _require(top_id.dim() == 2, "top_id: matrix [N,K] required")
     (N, V), K, dev, f32 = logits.shape, top_id.shape[1], logits.device, torch.float32
     rows = logits.shape[:1]
-    dlogits = logits.new_empty((N, V)) if dlogits is None else dlogits
-    loss = logits.new_empty(1, dtype=f32) if loss is None else loss
-    row_loss = logits.new_empty(rows, dtype=f32) if row_loss is None else row_loss
-    d, dld = _logit_rows(dlogits, "dlogits", logits)
+    if dlogits is None:
+        dlogits = logits.new_empty((N, V))
+        d, dld = dlogits.data_ptr(), V
+    else:
+        d, dld = _logit_rows(dlogits, "dlogits", logits)
+    # (one array for both: loss first)
+    if loss is None and row_loss is None:
+        loss, row_loss = logits.new_empty(N + 1, dtype=f32).split_with_sizes((1, N))
+        one = loss.data_ptr()
+        each = one + 4
+    else:
+        loss = logits.new_empty(1, dtype=f32) if loss is None else loss
+        row_loss = logits.new_empty(rows, dtype=f32) if row_loss is None else row_loss
+        one, each = _like(loss, dev, (1,), f32, "loss"), _like(row_loss, dev, rows, f32, "row_loss")
     _run(dev, lib.distill_topk_fwd_bwd, N, V, K, _dtype(logits), temperature, p, ld, _like(top_id, dev, (N, K), torch.int32, "top_id"),
-         _like(top_logit, dev, (N, K), f32, "top_logit"), _like(weight, dev, rows, f32, "weight"), _like(loss, dev, (1,), f32, "loss"),
-         _like(row_loss, dev, rows, f32, "row_loss"), d, dld)
+         _like(top_logit, dev, (N, K), f32, "top_logit"), _like(weight, dev, rows, f32, "weight"), one, each, d, dld)
     return loss, row_loss, dlogits
 
 
