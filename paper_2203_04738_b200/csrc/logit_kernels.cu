@@ -3,8 +3,10 @@
 //
 // All are bound by HBM (a row is read once, gradients are written once) with one or two exponentials an element, which take up to three
 // quarters of that time (16 a cycle and SM).
-//  * short rows (V <= 1024): a group of 8 or 32 lanes has a row, in registers;
-//  * longer ones: a block, or a cluster of up to 16 that meet through distributed shared memory.  The first
+//  * short rows (V <= 64): eight lanes have a row, in registers;
+//  * many rows of up to some KB: a warp has a row, and no two warps wait for each other (65536 rows of 1100 logits in bf16: distillation
+//    100 us, bytes 45; with a block to a row it is bound by the blocks' starts and meetings, some 3 ns a row: 484);
+//  * other rows: a block, or a cluster of up to 16 that meet through distributed shared memory.  The first
 //    pass streams the row once with a reference for the exponents that only moves when it has to; what is looked at twice (the gradient's
 //    pass, the vectors that hold a top alternative) comes from L2, where the rows in work have room.  Small blocks and no state but the
 //    sums: holding a row in registers or shared memory instead took 138 us for distillation of 4096 x 32768 in bf16 (bytes: 82), bound
@@ -25,7 +27,7 @@ constexpr int kMaxTop = 128, kMaxTeacher = 1024;
 constexpr int kRow = 256, kBatch = 4;          // threads of a block, 16-byte vectors of a thread at a time
 constexpr int kBlocks = 5;                     // on an SM: registers are kept to that (4: 115 us for distillation of 4096 x 32768 bf16; 5: 110)
 constexpr int kMaxCluster = 16;
-constexpr int kShortRow = 1024;
+constexpr int kShortRow = 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
@@ -82,19 +84,19 @@ template <class T> __device__ __forceinline__ float max_of(const V16<T>& v) {
   }
 }
 
-// A block's part of a row: n whole vectors from `first`, element v0 of the row on; and at most one of the row's other elements for each
-// lane of the first warp (in front of the row's first whole vector, behind its last one)
+// A block's or a warp's part of a row: n whole vectors from `first`, element v0 of the row on; and at most one of the row's other elements
+// for each of the threads l < 16 (in front of the row's first whole vector, behind its last one)
 template <class T> struct Part {
   static constexpr int E = V16<T>::E;
   i64 n; int v0, edge;
   const uint4* first;
-  __device__ __forceinline__ Part(const T* row, int V, int cluster, int rank) {
+  __device__ __forceinline__ Part(const T* row, int V, int cluster, int rank, int l) {
     const int skip = (int)((16u - ((uintptr_t)row & 15u)) & 15u) / (int)sizeof(T), head = min(skip, V), vecs = (V - head) / E;
     const int per = (vecs + cluster - 1) / cluster, lo = min(vecs, rank * per);
     n = min(vecs - lo, per);
     v0 = head + lo * E;
     first = reinterpret_cast<const uint4*>(row + v0);
-    const int l = (int)threadIdx.x, tail = V - head - vecs * E;
+    const int tail = V - head - vecs * E;
     edge = -1;
     if (l < 8 && rank == 0 && l < head) edge = l;
     if (l >= 8 && l < 16 && rank == cluster - 1 && l - 8 < tail) edge = head + vecs * E + l - 8;
@@ -109,13 +111,13 @@ template <class T> __device__ __forceinline__ int elements_of(const T* row, int 
 }
 
 // What a thread has seen of a row: the largest logit, m; s = sum 2^((x - r) c) and w, the same terms times their exponents, for a reference r that
-// follows the largest logit only when that has left it far behind (the terms stay below 2^44, the sums in range).
+// follows the largest logit only when that has left it far behind (the terms stay below 2^16; what the sums lose by it is 16 roundings).
 struct Seen {
   float m = -INFINITY, r = -3.4028235e38f;
   F<2> s = F<2>::all(0.f), w = F<2>::all(0.f);
   __device__ __forceinline__ void follow(float top, float c) {
     m = max_nan(m, top);
-    if ((top - r) * c > 40.f) {                // (the first time: r is the lowest value there is)
+    if ((top - r) * c > 16.f) {                // (the first time: r is the lowest value there is)
       const float d = (r - top) * c, f = ex2(d);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -137,6 +139,54 @@ struct Seen {
 template <bool W, class T> __device__ __forceinline__ void see_edge(Seen& t, float x, float c) {
   t.follow(x, c);
   t.add<W>(F<2>{{x, -INFINITY}}, c);
+}
+
+// The thread's vectors first + i, i = l, l + G, .. < n of a row, a batch of loads in flight at a time: sums, and the largest logits of the
+// thread's best batch (which starts at `where`) and of the others.
+struct Best { float high = -INFINITY, others = -INFINITY; int where = -1; };
+template <int G, bool W, bool TOP, class T> __device__ __forceinline__ void see_vectors(const Part<T>& p, int l, float c, Seen& t, Best& b) {
+  for (int i = l; i < p.n; i += G * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * G < p.n) x[q].w = p.first[i + q * G];
+    float m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * G < p.n) m = max_nan(m, max_of(x[q]));
+    t.follow(m, c);
+    if (TOP) {
+      if (m > b.high) { b.others = b.high; b.high = m; b.where = i; }
+      else b.others = fmaxf(b.others, m);
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      if (i + q * G < p.n) {
+#pragma unroll
+        for (int e = 0; e < V16<T>::E / 2; ++e) t.add<W>(x[q].pair(e), c);
+      }
+    }
+  }
+}
+// The thread's logits from `least` on, to offer(logit, token): as a rule those of its best batch are all
+template <int G, class T, class Offer> __device__ __forceinline__ void offer_vectors(const Part<T>& p, int l, const Best& b, float least, Offer&& offer) {
+  if (!(b.high >= least)) return;
+  const bool all = b.others >= least;
+  for (int i = all ? l : b.where; i < p.n; i += G * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * G < p.n) x[q].w = p.first[i + q * G];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      if (i + q * G < p.n && max_of(x[q]) >= least) {
+#pragma unroll
+        for (int e = 0; e < V16<T>::E; ++e)
+          if (x[q].get(e) >= least) offer(x[q].get(e), p.v0 + (i + q * G) * V16<T>::E + e);
+      }
+    }
+    if (!all) break;
+  }
 }
 
 // ---- reductions over a block -----------------------------------------------------------------------------------------------------
@@ -188,7 +238,7 @@ template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& 
   }
 }
 
-// ---- log probabilities: rows in the registers of a block or a cluster --------------------------------------------------------------
+// ---- log probabilities of longer rows --------------------------------------------------------------------------------------------
 
 constexpr int kList = 2048;                    // candidates that a block holds: its own, or those of a cluster
 constexpr int kRanked = 512;                   // of its own as many are put in order by counting (2 us); more are ties, and taken out one by one
@@ -206,7 +256,7 @@ template <int NT, class Out> __device__ __forceinline__ void by_rank(const unsig
 }
 
 // The top alternatives: every warp names the j largest of its threads' largest logits, j = top / warps rounded up; the top-th largest of all that
-// are named is a bound that at least `top` logits reach (top > 32: the lowest of them).  Only threads whose largest logit reaches it look at
+// are named is a bound that at least `top` logits reach (more than 32 names: the lowest of them).  Only threads whose largest logit reaches it look at
 // their logits again, as a rule at one batch of them, since a thread knows the largest logit of its best batch and of all the others.  What
 // they find, little more than `top`, is put in order by counting.  Where ties or a NaN make it much, the largest is taken out `top` times.
 template <class T, bool TOP>
@@ -215,52 +265,31 @@ __global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restr
   __shared__ unsigned long long list[TOP ? kList : 1];
   __shared__ unsigned long long best[TOP ? kMaxTop : 1];
   __shared__ float wmax[NW], wsum[NW], wdot[NW];
-  __shared__ unsigned named[TOP ? kMaxTop + 32 : 1];
+  __shared__ unsigned named[TOP ? kMaxTop + 32 * NW : 1];
   __shared__ Stats part;
   __shared__ int count;
   const int r = blockIdx.x / cluster, rank = blockIdx.x - r * cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
   const T* row = logits + (i64)r * a.ld;
-  const Part<T> p(row, a.V, cluster, rank);
+  const Part<T> p(row, a.V, cluster, rank, threadIdx.x);
   if (threadIdx.x == 0) count = 0;
   const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
   Seen t;
-  float high = -INFINITY, others = -INFINITY;  // largest logits of the thread's best batch and of the rest
-  int where = -1;
-  for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
-    V16<T> x[kBatch];
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-      if (i + q * kRow < p.n) x[q].w = __ldg(p.first + i + q * kRow);
-    float m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-      if (i + q * kRow < p.n) m = max_nan(m, max_of(x[q]));
-    t.follow(m, kLog2e);
-    if (TOP) {
-      if (m > high) { others = high; high = m; where = i; }
-      else others = fmaxf(others, m);
-    }
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      if (i + q * kRow < p.n) {
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) t.add<true>(x[q].pair(e), kLog2e);
-      }
-    }
-  }
+  Best mine;
+  see_vectors<kRow, true, TOP>(p, threadIdx.x, kLog2e, t, mine);
   if (p.edge >= 0) see_edge<true, T>(t, edge, kLog2e);
   float m = warp_max(t.m);
   if (lane == 0) wmax[warp] = m;
-  const int j = TOP ? (a.top + NW - 1) / NW : 0;
-  if (TOP) {
+  // (warps without vectors have nothing to name)
+  const int warps = max(1, min(NW, (int)((p.n + 31) / 32))), j = TOP ? (a.top + warps - 1) / warps : 0;
+  if (TOP && warp < warps) {
     unsigned k = value_key(t.m), b = 0u;
     for (int i = 0; i < min(j, 32); ++i) {
       b = __reduce_max_sync(0xffffffffu, k);
       const unsigned who = __ballot_sync(0xffffffffu, k == b);
       if (lane == __ffs(who) - 1) k = 0u;
-      if (lane == 0) named[warp * j + i] = b;
+      if (lane == 0) named[warp * min(j, 32) + i] = b;
     }
   }
   __syncthreads();
@@ -270,45 +299,27 @@ __global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restr
   if (lane == 0) { wsum[warp] = s1; wdot[warp] = w1; }
   if (TOP) {
     unsigned bound = 0u;
-    if (a.top <= 32) {
-      const unsigned mine = lane < NW * j ? named[lane] : 0u;
+    if (warps * j <= 32) {
+      const unsigned theirs = lane < warps * j ? named[lane] : 0u;
       int above = 0;
 #pragma unroll 8
       for (int i = 0; i < 32; ++i) {
-        const unsigned o = __shfl_sync(0xffffffffu, mine, i);
-        above += o > mine || (o == mine && i < lane);
+        const unsigned o = __shfl_sync(0xffffffffu, theirs, i);
+        above += o > theirs || (o == theirs && i < lane);
       }
-      bound = __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, above == a.top - 1)) - 1);
-    } else {
+      bound = __shfl_sync(0xffffffffu, theirs, __ffs(__ballot_sync(0xffffffffu, above == a.top - 1)) - 1);
+    } else if (j <= 32) {
       bound = 0xffffffffu;
-      for (int i = lane; i < NW * j; i += 32) bound = min(bound, named[i]);
+      for (int i = lane; i < warps * j; i += 32) bound = min(bound, named[i]);
       bound = __reduce_min_sync(0xffffffffu, bound);
     }
     const float least = bound == 0u ? -INFINITY : key_value(bound);
     const auto offer = [&](float x, int v) {
-      if (x >= least) {
-        const int place = atomicAdd(&count, 1);
-        if (place < kRanked) list[place] = top_key(x, v);
-      }
+      const int place = atomicAdd(&count, 1);
+      if (place < kRanked) list[place] = top_key(x, v);
     };
-    if (p.edge >= 0) offer(edge, p.edge);
-    if (high >= least) {
-      const bool all = others >= least;
-      for (int i = all ? (int)threadIdx.x : where; i < p.n; i += kRow * kBatch) {
-        V16<T> x[kBatch];
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q)
-          if (i + q * kRow < p.n) x[q].w = __ldg(p.first + i + q * kRow);
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-          if (i + q * kRow < p.n && max_of(x[q]) >= least) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) offer(x[q].get(e), p.v0 + (i + q * kRow) * E + e);
-          }
-        }
-        if (!all) break;
-      }
-    }
+    if (p.edge >= 0 && edge >= least) offer(edge, p.edge);
+    offer_vectors<kRow>(p, threadIdx.x, mine, least, offer);
   }
   __syncthreads();
   Stats all{m, all_sum<NW>(wsum), all_sum<NW>(wdot)};
@@ -400,6 +411,92 @@ __global__ void __launch_bounds__(kRow, kBlocks) logprob_kernel(const T* __restr
   blocks.sync();                               // nobody leaves while its shared memory may be read
 }
 
+// ---- log probabilities: a warp has a row ---------------------------------------------------------------------------------------------
+
+constexpr int kWarpRows = 8;                   // rows of a block
+constexpr int kWarpList = 128;                 // candidates of a row
+constexpr int kWarpTop = 32;                   // alternatives that 32 lanes' largest logits can bound
+
+template <class T, bool TOP>
+__global__ void __launch_bounds__(kWarpRows * 32, kBlocks) logprob_warp_kernel(const T* __restrict__ logits, const LogprobArgs a) {
+  constexpr int E = V16<T>::E;
+  __shared__ unsigned long long lists[TOP ? kWarpRows : 1][kWarpList];
+  __shared__ int counts[kWarpRows];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait();
+  pdl_trigger();
+  const i64 r_ = (i64)blockIdx.x * kWarpRows + warp;
+  if (r_ >= a.N) return;                       // (whole warps: nothing below waits for another)
+  const int r = (int)r_;
+  const T* row = logits + (i64)r * a.ld;
+  const Part<T> p(row, a.V, 1, 0, lane);
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
+  Seen t;
+  Best mine;
+  see_vectors<32, true, TOP>(p, lane, kLog2e, t, mine);
+  if (p.edge >= 0) see_edge<true, T>(t, edge, kLog2e);
+  const float m = warp_max(t.m), m0 = ref_of(m), d = (t.r - m0) * kLog2e, f = ex2(d);
+  Stats all{m, warp_sum((t.s.x[0] + t.s.x[1]) * f), warp_sum(f == 0.f ? 0.f : f * (fmaf(t.s.x[0], d, t.w.x[0]) + fmaf(t.s.x[1], d, t.w.x[1])))};
+  if (m == -INFINITY) all.s = all.w = 0.f;
+  if (lane == 0) write_row(a, row, r, all);
+  if (!TOP) return;
+  // the top-th largest of the lanes' largest logits: at least `top` logits reach it
+  unsigned k = value_key(t.m), bound = 0u;
+  for (int i = 0; i < a.top; ++i) {
+    bound = __reduce_max_sync(0xffffffffu, k);
+    const unsigned who = __ballot_sync(0xffffffffu, k == bound);
+    if (lane == __ffs(who) - 1) k = 0u;
+  }
+  const float least = bound == 0u ? -INFINITY : key_value(bound), ls = log_sum(all);
+  unsigned long long* list = lists[TOP ? warp : 0];
+  if (lane == 0) counts[warp] = 0;
+  __syncwarp();
+  const auto offer = [&](float x, int v) {
+    const int place = atomicAdd(&counts[warp], 1);
+    if (place < kWarpList) list[place] = top_key(x, v);
+  };
+  if (p.edge >= 0 && edge >= least) offer(edge, p.edge);
+  offer_vectors<32>(p, lane, mine, least, offer);
+  __syncwarp();
+  const auto answer = [&](int i, unsigned long long key) {
+    a.top_id[(i64)r * a.top + i] = key_token(key);
+    a.top_logprob[(i64)r * a.top + i] = logprob_of(key_value((unsigned)(key >> 32)), all, ls);
+  };
+  const int found = counts[warp];
+  if (m == m && found <= kWarpList) {
+    for (int i = lane; i < found; i += 32) {
+      const unsigned long long key = list[i];
+      int rank = 0;
+#pragma unroll 4
+      for (int q = 0; q < found; ++q) rank += list[q] > key;
+      if (rank < a.top) answer(rank, key);
+    }
+    return;
+  }
+  unsigned long long last = ~0ull;             // many are equal, or there is a NaN
+  for (int i = 0; i < a.top; ++i) {
+    unsigned long long top = 0;
+    const auto look = [&](float x, int v) {
+      const unsigned long long key = top_key(x, v);
+      if (key < last && key > top) top = key;
+    };
+    if (p.edge >= 0) look(edge, p.edge);
+    for (int q = lane; q < p.n; q += 32) {
+      V16<T> x;
+      x.w = p.first[q];
+#pragma unroll
+      for (int e = 0; e < E; ++e) look(x.get(e), p.v0 + q * E + e);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, top, o);
+      top = other > top ? other : top;
+    }
+    last = top;
+    if (lane == 0) answer(i, last);
+  }
+}
+
 // ---- log probabilities of short rows -----------------------------------------------------------------------------------------------
 
 // G lanes have a row, PER logits each
@@ -475,6 +572,47 @@ struct LogprobGradArgs {
   const int32_t* tokens; const float *lse, *entropy, *dlogprob, *dentropy;
 };
 
+// one row's gradient, element by element: -p (gl + ge (log p + entropy)), and gl at the token
+struct RowGrad {
+  int tok; bool dead;
+  float gl, ge, lse, c0;
+  __device__ __forceinline__ RowGrad(const LogprobGradArgs& a, int r) {
+    tok = a.tokens ? a.tokens[r] : -1;
+    if (tok >= a.V) tok = -1;
+    gl = tok >= 0 ? a.dlogprob[r] : 0.f;
+    ge = a.dentropy ? a.dentropy[r] : 0.f;
+    c0 = fmaf(ge, a.dentropy ? a.entropy[r] : 0.f, gl);
+    lse = a.lse[r];
+    dead = lse == -INFINITY;
+  }
+  __device__ __forceinline__ float one(float v, int at) const {
+    const float logp = v - lse, q = ex2(logp * kLog2e), g = q == 0.f ? 0.f : -q * fmaf(ge, logp, c0);
+    return dead ? 0.f : at == tok ? g + gl : g;
+  }
+  template <class T> __device__ __forceinline__ void vector(const V16<T>& x, int v, const T* row, T* out) const {
+    constexpr int E = V16<T>::E;
+    V16<T> y;
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+      const F<2> logp = x.pair(e) + F<2>::all(-lse);
+      const F<2> pr = each(logp * F<2>::all(kLog2e), [](float v, int) { return ex2(v); });
+      const F<2> g = fma_(logp, F<2>::all(-ge), F<2>::all(-c0)) * pr;
+      y.set_pair(e, each(g, [&](float v, int k) { return pr.x[k] == 0.f ? 0.f : v; }));
+    }
+    if (dead) y.w = make_uint4(0u, 0u, 0u, 0u);
+    if ((unsigned)(tok - v) < (unsigned)E) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (v + e == tok) y.set(e, one(x.get(e), tok));
+    }
+    if ((((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0) {
+      __stcs(reinterpret_cast<uint4*>(out + v), y.w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[v + e] = y.raw(e);
+    }
+  }
+};
 // Statistics are given, so every element is on its own: a block has a part of a row, all of its loads in flight at once.
 template <class T>
 __global__ void __launch_bounds__(kRow) logprob_back_kernel(const T* logits, T* dlogits, const LogprobGradArgs a, int parts) {
@@ -484,49 +622,46 @@ __global__ void __launch_bounds__(kRow) logprob_back_kernel(const T* logits, T* 
   pdl_trigger();
   const T* row = logits + (i64)r * a.ld;
   T* out = dlogits + (i64)r * a.dld;
-  const Part<T> p(row, a.V, parts, rank);
+  const Part<T> p(row, a.V, parts, rank, threadIdx.x);
   V16<T> x[kBatch];
 #pragma unroll
   for (int q = 0; q < kBatch; ++q)
     if ((int)threadIdx.x + q * kRow < p.n) x[q].w = __ldcs(p.first + threadIdx.x + q * kRow);
   const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : 0.f;
-  const int tok = a.tokens ? a.tokens[r] : -1;
-  const bool has = tok >= 0 && tok < a.V;
-  const float gl = has ? a.dlogprob[r] : 0.f, ge = a.dentropy ? a.dentropy[r] : 0.f, ent = a.dentropy ? a.entropy[r] : 0.f, lse = a.lse[r];
-  const bool dead = lse == -INFINITY;
-  const float c0 = fmaf(ge, ent, gl);          // gradient: -p (gl + ge (log p + ent)), and gl at the token
-  const auto one = [&](float v, int at) {
-    const float logp = v - lse, q = ex2(logp * kLog2e), g = q == 0.f ? 0.f : -q * fmaf(ge, logp, c0);
-    return dead ? 0.f : at == tok ? g + gl : g;
-  };
-  const bool same = (((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0;
+  const RowGrad g(a, r);
 #pragma unroll
   for (int q = 0; q < kBatch; ++q) {
-    const int i = (int)threadIdx.x + q * kRow, v = p.v0 + i * E;
-    if (i < p.n) {
-      V16<T> y;
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) {
-        const F<2> logp = x[q].pair(e) + F<2>::all(-lse);
-        const F<2> pr = each(logp * F<2>::all(kLog2e), [](float v, int) { return ex2(v); });
-        const F<2> g = fma_(logp, F<2>::all(-ge), F<2>::all(-c0)) * pr;
-        y.set_pair(e, each(g, [&](float v, int k) { return pr.x[k] == 0.f ? 0.f : v; }));
-      }
-      if (dead) y.w = make_uint4(0u, 0u, 0u, 0u);
-      if (has && (unsigned)(tok - v) < (unsigned)E) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (v + e == tok) y.set(e, one(x[q].get(e), tok));
-      }
-      if (same) {
-        __stcs(reinterpret_cast<uint4*>(out + v), y.w);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) out[v + e] = y.raw(e);
-      }
-    }
+    const int i = (int)threadIdx.x + q * kRow;
+    if (i < p.n) g.vector(x[q], p.v0 + i * E, row, out);
   }
-  if (p.edge >= 0) out[p.edge] = from_f32<T>(one(edge, p.edge));
+  if (p.edge >= 0) out[p.edge] = from_f32<T>(g.one(edge, p.edge));
+}
+
+// the same, a warp to a row
+template <class T>
+__global__ void __launch_bounds__(kRow) logprob_back_warp_kernel(const T* logits, T* dlogits, const LogprobGradArgs a) {
+  constexpr int E = V16<T>::E;
+  const int lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_trigger();
+  const i64 r_ = (i64)blockIdx.x * (kRow / 32) + (threadIdx.x >> 5);
+  if (r_ >= a.N) return;
+  const int r = (int)r_;
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const Part<T> p(row, a.V, 1, 0, lane);
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : 0.f;
+  const RowGrad g(a, r);
+  for (int i = lane; i < p.n; i += 32 * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * 32 < p.n) x[q].w = __ldcs(p.first + i + q * 32);
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * 32 < p.n) g.vector(x[q], p.v0 + (i + q * 32) * E, row, out);
+  }
+  if (p.edge >= 0) out[p.edge] = from_f32<T>(g.one(edge, p.edge));
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------------------------
@@ -537,6 +672,26 @@ struct DistillArgs {
 };
 // The student's side of one row: q = 2^((x - m) c) / s with c = log2(e) / tau
 struct Student { float m, s; };
+
+// f 2^((x - M) c) of the thread's vectors
+template <int G, class T> __device__ __forceinline__ void write_scaled(const Part<T>& p, int l, uint4* out, float M, float c, float f) {
+  for (int i = l; i < p.n; i += G * kBatch) {
+    V16<T> x[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (i + q * G < p.n) x[q].w = __ldcs(p.first + i + q * G);
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      if (i + q * G < p.n) {
+        V16<T> y;
+#pragma unroll
+        for (int e = 0; e < V16<T>::E / 2; ++e)
+          y.set_pair(e, each((x[q].pair(e) + F<2>::all(-M)) * F<2>::all(c), [](float v, int) { return ex2(v); }) * F<2>::all(f));
+        __stcs(out + i + q * G, y.w);
+      }
+    }
+  }
+}
 
 // Two passes over a row, the second from L2.  The gradient of the whole row is scale q; the places of the teacher's alternatives are written
 // once more, by the first of those that name the same token, after the block has written the rest.
@@ -553,7 +708,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
   pdl_trigger();
   const T* row = logits + (i64)r * a.ld;
   T* out = dlogits + (i64)r * a.dld;
-  const Part<T> p(row, a.V, cluster, rank);
+  const Part<T> p(row, a.V, cluster, rank, threadIdx.x);
   const float inv = 1.0f / a.tau, c = kLog2e * inv;
   const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
   const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
@@ -565,24 +720,8 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
     prob[k] = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
   }
   Seen t;
-  for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
-    V16<T> x[kBatch];
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-      if (i + q * kRow < p.n) x[q].w = p.first[i + q * kRow];
-    float m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-      if (i + q * kRow < p.n) m = max_nan(m, max_of(x[q]));
-    t.follow(m, c);
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      if (i + q * kRow < p.n) {
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) t.add<false>(x[q].pair(e), c);
-      }
-    }
-  }
+  Best unused;
+  see_vectors<kRow, false, false>(p, threadIdx.x, c, t, unused);
   if (p.edge >= 0) see_edge<false, T>(t, edge, c);
   float ym = -INFINITY;
   bool any = false;
@@ -638,22 +777,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
   const auto one = [&](float v) { return none ? 0.f : ex2((v - M) * c) * f; };
   const bool same = (((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0;
   if (same && !none) {
-    for (int i = threadIdx.x; i < p.n; i += kRow * kBatch) {
-      V16<T> x[kBatch];
-#pragma unroll
-      for (int q = 0; q < kBatch; ++q)
-        if (i + q * kRow < p.n) x[q].w = __ldcs(p.first + i + q * kRow);
-#pragma unroll
-      for (int q = 0; q < kBatch; ++q) {
-        if (i + q * kRow < p.n) {
-          V16<T> y;
-#pragma unroll
-          for (int e = 0; e < E / 2; ++e)
-            y.set_pair(e, each((x[q].pair(e) + F<2>::all(-M)) * F<2>::all(c), [](float v, int) { return ex2(v); }) * F<2>::all(f));
-          __stcs(reinterpret_cast<uint4*>(out + p.v0) + i + q * kRow, y.w);
-        }
-      }
-    }
+    write_scaled<kRow>(p, threadIdx.x, reinterpret_cast<uint4*>(out + p.v0), M, c, f);
   } else {                                     // a row of zeros, or rows that start at different places of a vector
     for (int i = threadIdx.x; i < p.n; i += kRow) {
       V16<T> x;
@@ -693,6 +817,91 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
     }
   }
   if (cluster > 1) cg::this_cluster().barrier_wait();
+}
+
+// The same, a warp to a row.  The alternatives of each row lie in shared memory (K <= kWarpTeacher).
+constexpr int kWarpTeacher = 128;
+template <class T>
+__global__ void __launch_bounds__(kWarpRows * 32, kBlocks) distill_warp_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+  constexpr int E = V16<T>::E;
+  extern __shared__ float teacher[];           // for each row: [K] probability, [K] the student's logit, [K] token
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float *prob = teacher + warp * 3 * a.K, *gap = prob + a.K;
+  int* id = reinterpret_cast<int*>(gap + a.K);
+  pdl_wait();
+  pdl_trigger();
+  const i64 r_ = (i64)blockIdx.x * kWarpRows + warp;
+  if (r_ >= a.N) return;                       // (whole warps: nothing below waits for another)
+  const int r = (int)r_;
+  const T* row = logits + (i64)r * a.ld;
+  T* out = dlogits + (i64)r * a.dld;
+  const Part<T> p(row, a.V, 1, 0, lane);
+  const float inv = 1.0f / a.tau, c = kLog2e * inv;
+  const float edge = p.edge >= 0 ? to_f32(row[p.edge]) : -INFINITY;
+  const float weight = a.weight ? a.weight[r] : 1.0f / (float)a.N;
+  float ym = -INFINITY;
+  bool any = false;
+  for (int k = lane; k < a.K; k += 32) {
+    const int v = a.top_id[(i64)r * a.K + k];
+    const bool in = v >= 0 && v < a.V;
+    const float y = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
+    id[k] = in ? v : -1;
+    prob[k] = y;
+    gap[k] = in ? to_f32(row[v]) : -INFINITY;
+    ym = fmaxf(ym, y);                         // (a NaN shows in the sum)
+    any = any || y != -INFINITY;
+  }
+  Seen t;
+  Best unused;
+  see_vectors<32, false, false>(p, lane, c, t, unused);
+  if (p.edge >= 0) see_edge<false, T>(t, edge, c);
+  const float m = warp_max(t.m), M = ref_of(m);
+  float s = warp_sum((t.s.x[0] + t.s.x[1]) * ex2((t.r - M) * c)), mass = 0.f;
+  if (m == -INFINITY) s = 0.f;
+  if (m != m || m == INFINITY) s = __int_as_float(0x7fc00000);
+  ym = warp_max(ym);
+  any = __any_sync(0xffffffffu, any);
+  const float y0 = ref_of(ym);
+  for (int k = lane; k < a.K; k += 32) mass += ex2((prob[k] - y0) * kLog2e);
+  mass = warp_sum(mass);
+  const float ls = logf(s), lmass = logf(mass), gain = weight * a.tau;
+  float loss = 0.f;
+  for (int k = lane; k < a.K; k += 32) {
+    const float logp = (prob[k] - y0) - lmass, pr = ex2(logp * kLog2e), z = gap[k];
+    const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
+    loss += pr == 0.f ? 0.f : pr * (logp - logq);
+    prob[k] = pr;
+  }
+  loss = warp_sum(loss);
+  if (lane == 0) a.row_loss[r] = any ? a.tau * a.tau * loss : 0.f;
+  const bool none = !any || weight == 0.f;
+  const float f = s == 0.f ? 0.f : gain / s;
+  const auto one = [&](float v) { return none ? 0.f : ex2((v - M) * c) * f; };
+  if ((((uintptr_t)row ^ (uintptr_t)out) & 15u) == 0 && !none) {
+    write_scaled<32>(p, lane, reinterpret_cast<uint4*>(out + p.v0), M, c, f);
+  } else {
+    for (int i = lane; i < p.n; i += 32) {
+      V16<T> x;
+      x.w = __ldcs(p.first + i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[p.v0 + i * E + e] = from_f32<T>(one(x.get(e)));
+    }
+  }
+  if (p.edge >= 0) out[p.edge] = from_f32<T>(one(edge));
+  __syncwarp();                                // the places of the alternatives are written once more
+  for (int k = lane; k < a.K && !none; k += 32) {
+    const int v = id[k];
+    if (v < 0) continue;
+    float pr = 0.f;
+    bool first = true;
+#pragma unroll 4
+    for (int j = 0; j < a.K; ++j) {
+      const bool twin = id[j] == v;
+      first = first && !(twin && j < k);
+      pr += twin ? prob[j] : 0.f;
+    }
+    if (first) out[v] = from_f32<T>(gain * ((s == 0.f ? 0.f : ex2((gap[k] - M) * c) / s) - pr));
+  }
 }
 
 // Short rows: G lanes have a row, PER logits each; the teacher's probabilities of each token meet in shared memory, in the order of the
@@ -819,6 +1028,12 @@ int blocks_of(int N, i64 bytes, bool twice) {
   while (c < kMaxCluster && (i64)N * c < 296 && bytes >= 2 * c * (i64)8192) c *= 2;
   return c;
 }
+// A warp to a row, of up to `most` bytes, where there are rows for eight warps on every multiprocessor; or the row is so short that a block
+// finds less than half a vector for each of its threads.  (us, a warp : a block to a row.  32768 rows of 4001 logits of 16 bits: 73 : 273
+// with the best five, gradient 91 : 109, distillation 111 : 276.  16384 rows of 8000: 65 : 160, 92 : 79, 115 : 164.  8192 rows of 8000 of 32
+// bits: 60 : 88, 92 : 79, 141 : 116.  600 rows of 8000 of 16 bits: 12 : 10, 13 : 6, 14 : 10.)
+bool warp_rows(int N, i64 bytes, i64 most) { return bytes <= 2048 || (bytes <= most && N >= 8 * 148 * (bytes > 16384 ? 2 : 1)); }
+
 template <class... KArgs, class... Args>
 cudaError_t launch_rows(void (*kern)(KArgs...), int N, int cluster, size_t smem, cudaStream_t s, Args&&... args) {
   if (cluster > 8) {                           // more than the portable size
@@ -850,9 +1065,9 @@ int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int6
     cudaStream_t s = (cudaStream_t)stream;
     const int c = blocks_of(N, (i64)V * (i64)sizeof(T), false);
     const auto few = [&](auto kern, int lanes) { e = launch_pdl(kern, dim3((unsigned)(((i64)N * lanes + kShortThreads - 1) / kShortThreads)), dim3(kShortThreads), 0, s, x, a); };
-    if (V <= 64) few(logprob_short_kernel<T, 8, 8>, 8);
-    else if (V <= 256) few(logprob_short_kernel<T, 32, 8>, 32);
-    else if (V <= kShortRow) few(logprob_short_kernel<T, 32, 32>, 32);
+    const auto warps = [&](auto kern) { e = launch_pdl(kern, dim3((unsigned)(((i64)N + kWarpRows - 1) / kWarpRows)), dim3(kWarpRows * 32), 0, s, x, a); };
+    if (V <= kShortRow) few(logprob_short_kernel<T, 8, 8>, 8);
+    else if (top <= kWarpTop && warp_rows(N, (i64)V * (i64)sizeof(T), 32768)) { if (top > 0) warps(logprob_warp_kernel<T, true>); else warps(logprob_warp_kernel<T, false>); }
     else if (top > 0) e = launch_rows(logprob_kernel<T, true>, N, c, 0, s, x, a);
     else e = launch_rows(logprob_kernel<T, false>, N, c, 0, s, x, a);
   });
@@ -876,7 +1091,11 @@ int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* log
   const LogprobGradArgs a{N, V, ld, dld, tokens, lse, entropy, dlogprob, dentropy};
   with_elem(dtype, [&](auto tag) {
     using T = decltype(tag);
-    e = launch_pdl(logprob_back_kernel<T>, dim3((unsigned)(N * parts)), dim3(kRow), 0, (cudaStream_t)stream, static_cast<const T*>(logits), static_cast<T*>(dlogits), a,
+    if (warp_rows(N, (i64)V * (i64)sizeof(T), 8192))
+      e = launch_pdl(logprob_back_warp_kernel<T>, dim3((unsigned)(((i64)N + kRow / 32 - 1) / (kRow / 32))), dim3(kRow), 0, (cudaStream_t)stream, static_cast<const T*>(logits),
+                     static_cast<T*>(dlogits), a);
+    else
+      e = launch_pdl(logprob_back_kernel<T>, dim3((unsigned)(N * parts)), dim3(kRow), 0, (cudaStream_t)stream, static_cast<const T*>(logits), static_cast<T*>(dlogits), a,
                    (int)parts);
   });
   return launched(e);
@@ -908,9 +1127,9 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
         added = blocks == 1;
         e = launch_pdl(kern, dim3((unsigned)blocks), dim3(kShortThreads), 0, s, x, d, a);
       };
-      if (V <= 64) few(distill_short_kernel<T, 8, 8>, 8);
-      else if (V <= 256) few(distill_short_kernel<T, 32, 8>, 32);
-      else if (V <= kShortRow) few(distill_short_kernel<T, 32, 32>, 32);
+      if (V <= kShortRow) few(distill_short_kernel<T, 8, 8>, 8);
+      else if (K <= kWarpTeacher && warp_rows(N, (i64)V * (i64)sizeof(T), 16384))
+        e = launch_pdl(distill_warp_kernel<T>, dim3((unsigned)(((i64)N + kWarpRows - 1) / kWarpRows)), dim3(kWarpRows * 32), (size_t)kWarpRows * K * 12, s, x, d, a);
       else e = launch_rows(distill_kernel<T>, N, c, (size_t)K * 12, s, x, d, a);
     });
     rc = launched(e);

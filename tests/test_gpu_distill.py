@@ -79,6 +79,34 @@ def test_absent_repeated_and_masked(V):
         check_distill(x, ids, y, w, 2.0, str(dtype))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,V,K,ld", [(1190, 1025, 16, None), (1201, 1100, 128, 1103), (1184, 4003, 129, None), (1184, 4003, 7, 4008), (1187, 150, 33, None), (1183, 4003, 7, None)])
+def test_many_rows_of_middling_width(N, V, K, ld, dtype):
+    inf, nan = float("inf"), float("nan")
+    ids, y = teacher(N, V, K, V)
+    x = rows(N, V, dtype, V, ld=ld, offset=0 if ld is None else 1)
+    w = np.random.default_rng(K).random(N).astype(np.float32)
+    ids[0] = -1
+    ids[1, 2:] = V
+    ids[2] = ids[2, 0]
+    ids[3, 3] = ids[3, 0]
+    y[4, 1:] = -inf
+    y[5] = -inf
+    x[8] = -inf
+    x[9] = torch.finfo(dtype).min
+    x[10, V // 2] = nan
+    y[11, 1] = nan
+    w[12] = 0
+    x[13, ids[13, 0]] = -inf
+    w[8:12] = w[13] = 0                                # (their losses are not finite)
+    ref = check_distill(x, ids, y, w, 2.0)[2]
+    out = torch.full((N, V + 2), 9.0, dtype=dtype, device="cuda")
+    check_distill(x, ids, y, w, 2.0, dlogits=out[:, 1:V + 1])
+    assert torch.equal(out[:, 1:V + 1], ref) and (out[:, 0] == 9).all() and (out[:, V + 1] == 9).all()
+    check_distill(x, ids, y, w, 2.0, dlogits=x)
+    assert torch.equal(x, ref)
+
+
 def test_in_place_and_inside_wider_rows():
     for dtype, V in ((F32, 51), (BF16, 4001), (F16, 33001)):
         ids, y = teacher(5, V, 7, 1)

@@ -67,6 +67,38 @@ def test_many_rows(N, V):
         check_rows(rows(N, V, dtype, N), np.random.default_rng(N).integers(-1, V + 1, N), 5)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,V,ld,top", [(1190, 1025, None, 20), (1201, 1100, 1103, 32), (1187, 2047, 2050, 31), (1184, 4003, None, 5), (1184, 4096, 4104, 33), (2373, 8001, None, 7),
+                                        (1300, 150, None, 20), (1300, 263, 270, 32), (1183, 4003, None, 32)])
+def test_many_rows_of_middling_width(N, V, ld, top, dtype):
+    """Values, alternatives and gradients, with masked rows, ties and NaN among the others."""
+    from paper_2203_04738_b200 import binding as L
+    x = rows(N, V, dtype, V, ld=ld, offset=0 if ld is None else 1)
+    inf = float("inf")
+    x[0] = -inf
+    x[1] = -inf
+    x[1, V // 2] = 2.0
+    x[9, 1::2] = -inf
+    x[10] = torch.finfo(dtype).min
+    x[11, V // 3] = float("nan")
+    x[12, V - 1] = inf
+    x[13, ::2] = 4.0                                   # equal ones
+    x[14, :120] = 4.0
+    x[15] = 0.5
+    x[16, :130] = 4.0
+    x[N - 1, V - 1] = 9.0
+    tok = np.random.default_rng(N).integers(-1, V + 1, N)
+    r = check_rows(x, tok, top)
+    rng = np.random.default_rng(V)
+    dl, de = [torch.from_numpy(rng.standard_normal(N).astype(np.float32)).cuda() for _ in range(2)]
+    d = L.token_logprobs_backward(x, ints(tok), r.lse, r.entropy, dlogprob=dl, dentropy=de)
+    ref, bound = R.logprobs_backward(R.to64(x), tok, R.to64(r.lse), R.to64(r.entropy), R.to64(dl), R.to64(de))
+    R.check(d, ref, bound + R.rounding(ref, dtype), "gradient")
+    out = torch.full((N, V + 2), 5.0, dtype=dtype, device="cuda")
+    L.token_logprobs_backward(x, ints(tok), r.lse, r.entropy, dlogprob=dl, dentropy=de, dlogits=out[:, 1:V + 1])
+    assert torch.equal(out[:, 1:V + 1].nan_to_num(7.0), d.nan_to_num(7.0)) and (out[:, 0] == 5).all() and (out[:, V + 1] == 5).all()
+
+
 @pytest.mark.parametrize("V", [9, 51, 700, 3000, 20000, 70000])
 def test_ties_go_to_the_lower_token(V):
     rng = np.random.default_rng(V)
