@@ -1,660 +1,17 @@
-// Gated linear recurrence h_t = a_t h_{t-1} + b_t, forward and backward.
-//
-// Every column (b, unit) is a recurrence of its own, so a column is a chain of T dependent multiply-adds over data that is read once:
-// bound by HBM as long as enough of the time axis is in flight at once.  Two kernels:
-//
-//  * scan_short_kernel, T <= kShort: a thread walks its columns.  One step of generation is this kernel: a launch and a trip to memory.
-//  * scan_tile_kernel: the time axis is cut into tiles of S x kWarps steps and 32 x VC columns.  A thread holds S steps of VC
-//    columns in registers from the only time they are read to the time the results are written.  It reduces them to one pair
-//    (A, B): h_out = A h_in + B; the pairs of a tile's warps meet in shared memory, those of the tiles in the workspace.  A tile
-//    publishes its pair as soon as it has it; the state in front of a tile is the last published state before it, carried
-//    through the pairs of the tiles in between (decoupled look-back), and is published in turn.  Blocks stay and take tiles from a
-//    counter, earlier times first, each in the order in which it got them: the first unfinished tile waits for nothing, so every wait
-//    ends; it is bounded all the same.  While a block works on a tile the loads of its next one are in flight.
-//    The state is carried through the pairs one after the other, by the operation that the tiles themselves would have used, so that the
-//    bits do not depend on how far a tile had to look back.
-//    Published words are their own flags: the workspace is filled with a bit pattern that no result has, a word that
-//    differs from it is there.  So publishing is a plain store and looking one trip to L2, without fences.
-//
-// Backward is the same scan from the last step to the first: mu_t = a_t (seed_t + mu_{t+1}).
-//
-// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 116 (61), backward 196 (123);
-// 65536 steps of 1024 units in fp32 forward 257 (123); one step of 32 x 1024 4.4.  What bounds it: two warps on each scheduler that issue
-// dependent arithmetic (42 % of the issue slots, exponentials and reciprocals 40 % of theirs, DRAM 39 %); with given coefficients the first
-// takes 80.  Few columns: the chain of tiles, 0.13 us each at 512 tiles.
-#include <type_traits>
-
-#include "elem.cuh"
+// Gated linear recurrence: arguments, workspace, status word and entry points.  The kernels are in scan_tile.cuh, compiled for one element type
+// at a time.
+#include "scan_tile.cuh"
 
 namespace mg {
+
+extern template int launch_scan<float>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__half>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
+
 namespace {
 
 __device__ int g_scan_status = 0;              // 1: a look-back's wait ran out
 int* g_scan_status_ptrs[kMaxDevices] = {nullptr};
-
-struct ScanRows { char* p; i64 ts, bs; };      // strides in elements
-struct ScanArgs {
-  int T, B, H, Hp;                             // Hp: H rounded up to whole threads (tile kernel)
-  float dt, K, L;                              // gate: q = dt / (K + E), a = (L + E) / (K + E); see coefficients()
-  ScanRows gate, cand, h, seed, dgate, dcand, reset;
-  const float* h0; const int32_t* lengths; float* hT;
-  const float* dhT; float* dh0;
-  // tiles: nk along time, nc along the columns
-  int nk, nc, deep;
-  unsigned* ticket; float* states; unsigned long long* pairs; int* status;      // [nk][nc * 32 VC] each
-};
-
-constexpr int kShort = 8;                      // steps that one thread walks
-constexpr int kShortThreads = 128;
-constexpr int kWarps = 8;
-template <class T> constexpr int kWide = 8 / sizeof(T);      // VC, columns of a thread: 8 bytes of a row
-// S, steps of a thread.  ALIGNED rows are staged in shared memory, others in registers.  Long pieces pay: what a tile costs whatever its
-// size (its place, the pairs of the other warps, one meeting, one look at L2) is shared by 64 elements of a thread, and the chain of tiles is
-// short.  One block fills an SM's registers.  Half the steps and two blocks: 116 -> 134 us forward, 196 -> 243 backward for T 2048, B 32,
-// H 1024 in bf16, 257 -> 323 for 65536 steps of 1024 units in fp32.
-template <bool ALIGNED, bool BACK> constexpr int kStepsOf = (ALIGNED ? 16 : 8) / (BACK ? 2 : 1);
-constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2: 122 us for the 116 above)
-constexpr int kLook = 4;                       // looks of 32 tiles back
-constexpr int kFirst = 2, kMore = 16;          // pairs in flight in a look-back: of a column at first, of the thread's columns then
-constexpr int kNarrow = 8;                     // column tiles up to which one warp looks back for its block
-constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
-constexpr float kMaxDt = 1e18f;
-
-__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float rcp_exact(float x) { const float y = rcp(x); return fmaf(fmaf(-x, y, 1.0f), y, y); }      // one Newton step
-
-// VC consecutive elements of a row, moved as one word
-template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
-  T x[VC];
-  __device__ __forceinline__ F<VC> get() const {
-    F<VC> f;
-#pragma unroll
-    for (int i = 0; i < VC; ++i) f.x[i] = to_f32(x[i]);
-    return f;
-  }
-  __device__ __forceinline__ void set(const F<VC>& f) {
-#pragma unroll
-    for (int i = 0; i < VC; ++i) x[i] = from_f32<T>(f.x[i]);
-  }
-};
-// the same, no lower than -40 (gates) or no higher than 10 (candidates); NaN stays.  Two 16-bit values take one instruction.
-template <bool GATE> __device__ __forceinline__ float clamped(float v) { float y; if (GATE) asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-40.f)); else asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(10.f)); return y; }
-template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; if (GATE) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc220c220u)); else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x41204120u)); return y; }
-template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; if (GATE) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd100d100u)); else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x49004900u)); return y; }
-template <bool GATE, class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Vec<T, VC>& x) {
-  if constexpr (sizeof(T) == 2 && VC % 2 == 0) {
-    Vec<T, VC> y;
-    const unsigned* in = reinterpret_cast<const unsigned*>(&x);
-    unsigned* out = reinterpret_cast<unsigned*>(&y);
-#pragma unroll
-    for (int i = 0; i < VC / 2; ++i) out[i] = clamped2<GATE>(in[i], T{});
-    return y.get();
-  } else {
-    F<VC> f = x.get();
-#pragma unroll
-    for (int i = 0; i < VC; ++i) f.x[i] = clamped<GATE>(f.x[i]);
-    return f;
-  }
-}
-template <class T, int VC> __device__ __forceinline__ Vec<T, VC> load(const T* p) { return *reinterpret_cast<const Vec<T, VC>*>(p); }
-template <class T, int VC> __device__ __forceinline__ void store(T* p, F<VC> f) {
-  Vec<T, VC> v;
-  v.set(f);
-  *reinterpret_cast<Vec<T, VC>*>(p) = v;
-}
-template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
-  Vec<T, VC> v;
-  v.set(F<VC>::all(0.f));
-  return v;
-}
-// The coefficients, and what their derivatives need.  With E = e^-g, G = e^2c and z = 1 / (1 + E):
-//   n = (G - 1) / (G + 1),  q = dt / (K + E),  a = 1 - q = (L + E) / (K + E),  b = q n
-// is the classic cell (q = dt z) for K = 1, L = 1 - dt and the implicit one (q = dt z / (1 + dt z)) for K = 1 + dt, L = 1, and in both
-//   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2).
-// Small candidates take the first terms of the tangent's series, since G - 1 would lose their digits.  E stops at e^40 and G at e^20,
-// where z is 4e-18 and n is 1.
-// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, the series' first term for |c| < 2^-9 (left out: 1.3e-6 of the
-// value).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
-// bytes 61).  The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
-// coefficients are right to a few units in the last place; two terms of the series for |c| < 0.1 (left out: 5e-8).
-template <int VC> struct Coef { F<VC> a, b, q, n, e; };      // e = E / (K + E)
-template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
-  constexpr bool FAST = sizeof(T) == 2;
-  Coef<VC> o;
-  using V = F<VC>;
-  if (GIVEN) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = V::all(0.f); return o; }
-  const V one = V::all(1.0f), g = get_clamped<true>(graw), c = get_clamped<false>(craw);
-  const V E = each(g * V::all(-1.44269504f), [](float v, int) { return ex2(v); }), G = each(c * V::all(2.88539008f), [](float v, int) { return ex2(v); });
-  const V P = E + V::all(s.K), Q = G + one;
-  V ip, iq;
-  if (FAST) {
-    const V R = each(P * Q, [](float v, int) { return rcp(v); });
-    ip = Q * R;
-    iq = P * R;
-  } else {
-    ip = each(P, [](float v, int) { return rcp_exact(v); });
-    iq = each(Q, [](float v, int) { return rcp_exact(v); });
-  }
-  o.n = (G + V::all(-1.0f)) * iq;
-  if (FAST) {
-    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.001953125f ? c.at(i) : v; });
-  } else {
-    const V c2 = c * c, small = c * fma_(c2, fma_(c2, V::all(0.13333334f), V::all(-0.33333334f)), one);
-    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.1f ? small.at(i) : v; });
-  }
-  o.q = ip * V::all(s.dt);
-  o.a = FAST ? fma_(o.q, V::all(-1.0f), one) : (E + V::all(s.L)) * ip;
-  o.b = o.q * o.n;
-  o.e = E * ip;
-  return o;
-}
-// d(gate), d(cand) of a step whose state has the derivative 1
-template <bool GIVEN, int VC> __device__ __forceinline__ void slopes(const Coef<VC>& k, F<VC> hp, F<VC>& wg, F<VC>& wc) {
-  using V = F<VC>;
-  if (GIVEN) { wg = hp; wc = V::all(1.0f); return; }
-  wg = (k.q * k.e) * fma_(hp, V::all(-1.0f), k.n);
-  wc = k.q * (fma_(k.n, V::all(-1.0f), V::all(1.0f)) * (k.n + V::all(1.0f)));
-}
-
-// n of VC states (the others are zero, or not stored)
-template <int VC> __device__ __forceinline__ F<VC> load_state(const float* p, unsigned col, int n = VC) {
-  F<VC> f;
-#pragma unroll
-  for (int v = 0; v < VC; ++v) f.at(v) = p && v < n ? p[col + v] : 0.f;
-  return f;
-}
-template <int VC> __device__ __forceinline__ void store_state(float* p, unsigned col, const F<VC>& f, int n = VC) {
-#pragma unroll
-  for (int v = 0; v < VC; ++v)
-    if (v < n) p[col + v] = f.at(v);
-}
-
-// What a thread knows of its columns: the first one, its sequence and unit, the steps of that sequence
-template <class T> struct Column {
-  unsigned col, b, u;
-  int len;
-  bool live;
-  __device__ __forceinline__ Column(const ScanArgs& a, unsigned c) : col(c) {
-    live = c < (unsigned)a.B * (unsigned)a.H;
-    b = live ? c / (unsigned)a.H : 0u;
-    u = live ? c - b * (unsigned)a.H : 0u;
-    len = !live ? 0 : a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-  }
-  __device__ __forceinline__ T* at(const ScanRows& r, int t) const { return reinterpret_cast<T*>(r.p) + (i64)t * r.ts + (i64)b * r.bs + u; }
-  __device__ __forceinline__ bool fresh(const ScanArgs& a, int t) const {
-    return reinterpret_cast<const uint8_t*>(a.reset.p)[(i64)t * a.reset.ts + (i64)b * a.reset.bs] != 0;
-  }
-};
-
-template <class T, bool GIVEN, int VC, bool BACK>
-__global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArgs a) {
-  using V = F<VC>;
-  const Column<T> q(a, (blockIdx.x * kShortThreads + threadIdx.x) * VC);
-  if (!q.live) return;
-  V h = load_state<VC>(BACK ? a.dhT : a.h0, q.col);
-  for (int i = 0; i < a.T; ++i) {
-    const int t = BACK ? a.T - 1 - i : i;
-    if (t >= q.len) {
-      store<T, VC>(q.at(BACK ? a.dgate : a.h, t), V::all(0.f));
-      if (BACK) store<T, VC>(q.at(a.dcand, t), V::all(0.f));
-      continue;
-    }
-    const bool fresh = a.reset.p && q.fresh(a, t);
-    const Coef<VC> k = coefficients<GIVEN, T, VC>(load<T, VC>(q.at(a.gate, t)), load<T, VC>(q.at(a.cand, t)), a);
-    if (BACK) {
-      const V hp = fresh ? V::all(0.f) : t > 0 ? load<T, VC>(q.at(a.h, t - 1)).get() : load_state<VC>(a.h0, q.col);
-      const V lam = a.seed.p ? h + load<T, VC>(q.at(a.seed, t)).get() : h;
-      V wg, wc;
-      slopes<GIVEN, VC>(k, hp, wg, wc);
-      store<T, VC>(q.at(a.dgate, t), lam * wg);
-      store<T, VC>(q.at(a.dcand, t), lam * wc);
-      h = fresh ? V::all(0.f) : k.a * lam;
-    } else {
-      h = fresh ? k.b : fma_(k.a, h, k.b);
-      store<T, VC>(q.at(a.h, t), h);
-    }
-  }
-  float* last = BACK ? a.dh0 : a.hT;
-  if (last) store_state<VC>(last, q.col, h);
-}
-
-// ---- words that tiles publish --------------------------------------------------------------------------------------------------
-
-constexpr unsigned kNone = 0xffffffffu;        // a NaN that no result is: NaN is published as 0x7fc00000
-__device__ __forceinline__ unsigned word_of(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
-__device__ __forceinline__ unsigned ld_word(const float* p) { unsigned v; asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v; }
-__device__ __forceinline__ void st_word(float* p, unsigned v) { asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" :: "l"(p), "r"(v) : "memory"); }
-__device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
-  unsigned long long v;
-  asm volatile("ld.relaxed.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
-}
-__device__ __forceinline__ void st_pair(unsigned long long* p, float2 v) {
-  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | word_of(v.x);
-  asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" :: "l"(p), "l"(w) : "memory");
-}
-__device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t)); return t; }
-
-// h through the pair p.  cut (some sequence starts anew somewhere): A = 0 cuts off what came before, whatever it was (0 x NaN would not).
-__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && p.x == 0.f ? p.y : fmaf(p.x, h, p.y); }
-__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(cut && p.x == 0.f ? 0.f : p.x * q.x, through(p, q.y, cut)); }
-
-// One round of a wait, for the whole warp: true once it has run out, here or elsewhere (the status word says so).
-__device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, unsigned round, uint64_t& t0) {
-  if ((round & 31u) != 31u) return false;
-  int stop = 0;
-  if (lane == 0) {
-    const uint64_t t = now_ns();
-    if (t0 == 0) t0 = t;
-    stop = *(volatile int*)a.status != 0;
-    if (!stop && t - t0 > kWaitNs) { atomicExch(a.status, 1); stop = 1; }
-  }
-  return __shfl_sync(0xffffffffu, stop, 0) != 0;
-}
-
-// The state in front of tile k of column tile c, for the warp's columns: carried from the last published state through the pairs after
-// it.  Words of a tile are published together, so one of them (the first column's) tells the lanes how far back to go.  A tile that found
-// the state in front of it at once publishes no pair, only its state: whoever misses a word looks again from the start.
-template <int VC, bool NARROW> __device__ __forceinline__ F<VC> look_back(const ScanArgs& a, int k, i64 row, i64 col, int lane) {
-  uint64_t t0 = 0;
-  for (unsigned round = 0; !waited_too_long(a, lane, round, t0); ++round) {
-    int from = -1;                             // the tile whose state is taken
-    int last = k - 1;
-#pragma unroll 1
-    for (int w = 0; w < kLook && last >= 0 && from < 0; ++w, last -= 32) {
-      const bool there = last - lane >= 0 && ld_word(a.states + (last - lane) * row + col) != kNone;
-      const unsigned m = __ballot_sync(0xffffffffu, there);
-      if (m) from = last - (__ffs(m) - 1);
-    }
-    if (from < 0) continue;
-    F<VC> h;
-    bool there = true;
-#pragma unroll
-    for (int v = 0; v < VC; ++v) {
-      const unsigned w = ld_word(a.states + from * row + col + lane * VC + v);
-      there = there && w != kNone;
-      h.at(v) = __uint_as_float(w);
-    }
-    // the pairs after it: two at first, which often are not there yet; NARROW: then many in one trip
-    const auto carry = [&](int j, auto pairs) {
-      constexpr int P = decltype(pairs)::value;
-      float2 p[P][VC];
-      const int n = min(P, k - j);
-      const unsigned long long* at = a.pairs + j * row + col + lane * VC;
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int v = 0; v < VC; ++v) p[i][v] = i < n ? ld_pair(at + i * row + v) : make_float2(1.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int v = 0; v < VC; ++v)
-          if (i < n) {
-            there = there && __float_as_uint(p[i][v].x) != kNone;
-            h.at(v) = through(p[i][v], h.at(v), a.reset.p != nullptr);
-          }
-      return j + P;
-    };
-    int j = from + 1;
-    if (NARROW && j + kFirst < k) {
-      j = carry(j, std::integral_constant<int, kFirst>{});
-#pragma unroll 1
-      while (j + kFirst < k && there) j = carry(j, std::integral_constant<int, kMore / VC>{});
-    }
-#pragma unroll 1
-    while (j < k && there) j = carry(j, std::integral_constant<int, kFirst>{});
-    if (__all_sync(0xffffffffu, there)) return h;
-  }
-  return F<VC>::all(__uint_as_float(0x7fc00000u));      // the results are void, and look it
-}
-
-// A tile's place, worked out by one thread for the block
-struct alignas(16) Place { int k, c; unsigned b, u; };      // chunk of time (-1: no tile), column tile; sequence and unit of its first column
-__device__ __forceinline__ Place place_of(const ScanArgs& a, unsigned tile, int columns) {
-  Place p;
-  if (tile >= (unsigned)a.nk * (unsigned)a.nc) return Place{-1, 0, 0u, 0u};
-  p.k = (int)(tile / (unsigned)a.nc);
-  p.c = (int)(tile - (unsigned)p.k * (unsigned)a.nc);
-  const unsigned col = (unsigned)p.c * (unsigned)columns;
-  p.b = col / (unsigned)a.Hp;
-  p.u = col - p.b * (unsigned)a.Hp;
-  return p;
-}
-
-template <class T, bool GIVEN, bool STAGED, bool BACK, bool NARROW>
-__global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
-  constexpr int VC = kWide<T>, S = kStepsOf<STAGED, BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
-  extern __shared__ __align__(16) char stage[];      // [tiles ahead][ARRAYS][S][threads] words of 8 bytes
-  constexpr unsigned ALL = (1u << S) - 1u;
-  using V = F<VC>;
-  __shared__ __align__(16) float2 pair[2][kWarps][CT];
-  constexpr int D = STAGED ? kAhead : 1, RING = 4;
-  static_assert(D < RING - 1, "a place is written while the one before it and those ahead are in use");
-  __shared__ Place place[RING];
-  __shared__ V front[NARROW ? 2 : 1][32];      // NARROW: the state in front of the tile
-  __shared__ volatile unsigned posted[2];      // ... and the turn whose state that is
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const i64 row = (i64)a.nc * CT;
-  const bool cut = a.reset.p != nullptr;
-  const auto time_of = [&](int i) { return BACK ? a.T - 1 - i : i; };
-
-  // where the thread stands in a tile: sequence and unit of its columns, its first step counted from the scan's start
-  struct Spot { unsigned b, u; int i0, n; };      // n: columns of the thread that exist
-  const auto spot_of = [&](const Place& p, int column) {
-    Spot s;
-    s.b = p.b;
-    s.u = p.u + column;
-    if (s.u >= (unsigned)a.Hp) {               // the tile reaches into the next sequences
-      const unsigned n = s.u / (unsigned)a.Hp;
-      s.b += n;
-      s.u -= n * (unsigned)a.Hp;
-    }
-    s.i0 = p.k * TT + warp * S;
-    s.n = s.b >= (unsigned)a.B ? 0 : STAGED ? VC : min(VC, a.H - (int)s.u);
-    return s;
-  };
-  const auto at = [&](const ScanRows& r, const Spot& s, int t) { return reinterpret_cast<T*>(r.p) + ((i64)t * r.ts + (i64)s.b * r.bs + s.u); };
-
-  // The warp's steps of a tile, as they come from memory.  Rows that allow it are staged in shared memory by asynchronous copies of 16
-  // bytes (two rows of a warp at a time, past L1), which leaves the registers to the tile in work; only the warp itself waits for them.
-  constexpr unsigned kRow = CT * sizeof(T), kPieces = kRow / 16, kRows = STAGED ? 32 / kPieces : 1;      // bytes of a row, copies of a row, rows at a time
-  constexpr unsigned kArray = S * kRow, kTile = kWarps * ARRAYS * kArray;
-  static_assert(!STAGED || (kRow % 16 == 0 && 32 % kPieces == 0 && S % kRows == 0), "whole copies of whole rows");
-  char* const slice = stage + warp * (ARRAYS * kArray);
-  const unsigned slot0 = (unsigned)__cvta_generic_to_shared(slice) + (lane / kPieces) * kRow + (lane % kPieces) * 16u;
-  Vec<T, VC> regs[STAGED ? 1 : ARRAYS][STAGED ? 1 : S];
-  const auto raw = [&](unsigned d, int array, int s) {
-    if (!STAGED) return regs[STAGED ? 0 : array][STAGED ? 0 : s];
-    return *reinterpret_cast<const Vec<T, VC>*>(slice + d * kTile + array * kArray + s * kRow + lane * sizeof(Vec<T, VC>));
-  };
-  // steps i0 .. i0 + S - 1 of the scan that lie in the sequence
-  const auto inside_of = [&](const Spot& s) {
-    const int len = s.n == 0 ? 0 : a.lengths ? min(max(a.lengths[s.b], 0), a.T) : a.T;
-    const int lo = BACK ? max(0, a.T - len - s.i0) : 0, hi = BACK ? min(S, a.T - s.i0) : min(S, len - s.i0);
-    return hi > lo ? (ALL >> (S - hi)) & (ALL << lo) : 0u;
-  };
-  // -> which of the thread's steps lie in the sequence, and (from bit 16 on) which of them start one
-  const auto fetch = [&](const Place& p, unsigned d) {
-    const Spot s = spot_of(p, lane * VC);
-    const unsigned inside = inside_of(s);
-    unsigned fresh = 0u;
-    const int t0 = time_of(s.i0);
-    if (cut) {                                 // all of them asked for before the first is looked at
-      uint8_t mark[S];
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const uint8_t* p = reinterpret_cast<const uint8_t*>(a.reset.p);
-        mark[i] = p[(inside >> i & 1u) ? (i64)time_of(s.i0 + i) * a.reset.ts + (i64)s.b * a.reset.bs : 0];
-      }
-#pragma unroll
-      for (int i = 0; i < S; ++i) fresh |= mark[i] && (inside >> i & 1u) ? 1u << i : 0u;
-    }
-    if constexpr (STAGED) {
-      const Spot mine = spot_of(p, (lane % kPieces) * (16 / (int)sizeof(T)));
-      const int r = (int)(lane / kPieces), t1 = BACK ? t0 - r : t0 + r;
-      const auto bring = [&](int array, const ScanRows& from, int t, bool there, auto whole) {
-        constexpr bool WHOLE = decltype(whole)::value;
-        const unsigned valid = WHOLE ? ALL : inside_of(mine);
-        const T* q = at(from, mine, t);
-        const i64 dq = (BACK ? -from.ts : from.ts) * (i64)kRows;
-        const unsigned to = slot0 + d * kTile + array * kArray;
-#pragma unroll
-        for (int i = 0; i < S / (int)kRows; ++i) {
-          if (WHOLE) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + i * (kRows * kRow)), "l"(q + i * dq) : "memory");
-          } else {                             // what lies outside is not read: zeros stand in for it
-            const int step = i * (int)kRows + r;
-            const bool in = there && (valid >> step & 1u) && (array != 2 || time_of(mine.i0 + step) > 0);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + i * (kRows * kRow)), "l"(in ? q + i * dq : reinterpret_cast<const T*>(a.gate.p)), "r"(in ? 16 : 0) : "memory");
-          }
-        }
-      };
-      if (__all_sync(0xffffffffu, inside == ALL && (!BACK || (t0 >= S && a.seed.p)))) {
-        bring(0, a.gate, t1, true, std::true_type{});
-        bring(1, a.cand, t1, true, std::true_type{});
-        if (BACK) { bring(2, a.h, t1 - 1, true, std::true_type{}); bring(3, a.seed, t1, true, std::true_type{}); }
-      } else {
-        bring(0, a.gate, t1, true, std::false_type{});
-        bring(1, a.cand, t1, true, std::false_type{});
-        if (BACK) { bring(2, a.h, t1 - 1, true, std::false_type{}); bring(3, a.seed, t1, a.seed.p != nullptr, std::false_type{}); }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    } else {
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const bool in = inside >> i & 1u;
-        const int t = time_of(s.i0 + i);
-        const auto take = [&](int array, const ScanRows& from, int t, bool there) {
-          Vec<T, VC> x = zeros<T, VC>();
-          const T* q = at(from, s, t);
-#pragma unroll
-          for (int v = 0; v < VC; ++v)
-            if (there && v < s.n) x.x[v] = q[v];
-          regs[array][i] = x;
-        };
-        take(0, a.gate, t, in);
-        take(1, a.cand, t, in);
-        if constexpr (BACK) {
-          take(2, a.h, t - 1, in && t > 0);
-          take(3, a.seed, t, in && a.seed.p);
-        }
-      }
-    }
-    return inside | fresh << 16;
-  };
-
-  if (NARROW && threadIdx.x < 2) posted[threadIdx.x] = 0u;      // (turns are counted from 1 there)
-  // Tiles are drawn from the counter (which starts at 2^32 - 1) by thread 32.  deep: D + 1 at the start, and from then on one round
-  // before a number is told to the others, so that nobody waits for it.  Otherwise (few tiles: they would all go to the first blocks)
-  // one at a time, and nothing is fetched ahead.
-  unsigned drawn = blockIdx.x - gridDim.x;
-  const auto draw = [&]() { return drawn = a.nk > 1 ? atomicAdd(a.ticket, 1u) + 1u : drawn + gridDim.x; };
-  const auto none = [&]() { if (STAGED) asm volatile("cp.async.commit_group;" ::: "memory"); return 0u; };
-  unsigned ahead[D];                           // what fetch() said of the tiles to come
-#pragma unroll
-  for (int i = 0; i < D; ++i) ahead[i] = 0u;
-  if (a.deep) {
-    if (threadIdx.x == 32) {
-      for (int i = 0; i <= D; ++i) place[i] = place_of(a, draw(), CT);
-      draw();
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < D; ++i) {
-      const Place p = place[i];
-      ahead[i] = p.k >= 0 ? fetch(p, i) : none();
-    }
-  }
-
-  // one tile; ODD: some step of the warp lies outside its sequence, starts a sequence or (backward) is the first one
-  const auto work = [&](auto odd_, unsigned d, unsigned turn, const Place& here, const Spot& now, unsigned in_now, unsigned fresh_now) {
-    constexpr bool ODD = decltype(odd_)::value;
-    const int k = here.k, c = here.c;
-    const unsigned buf = turn & 1u;
-    const i64 word = k * row + (i64)c * CT + lane * VC;
-    // The state in front: what the tile before has published, asked for early (it is usually there), or the first one, which every warp has
-    // read before the block meets, since the last tile may write its result over it (hT = h0).
-    unsigned early[VC];
-    if (k > 0) {
-#pragma unroll
-      for (int v = 0; v < VC; ++v) early[v] = ld_word(a.states + word - row + v);
-    } else {
-      const V first = load_state<VC>(BACK ? a.dhT : a.h0, now.b * (unsigned)a.H + now.u, now.n);
-#pragma unroll
-      for (int v = 0; v < VC; ++v) early[v] = __float_as_uint(first.at(v));
-    }
-    const unsigned told = drawn;
-    if (threadIdx.x == 32 && a.deep) draw();
-
-    V ca[S], cb[S], wg[SB], wc[SB];            // cb: b, backward: the seed
-    if (STAGED) asm volatile("cp.async.wait_group %0;" :: "n"(D - 1) : "memory");      // (all but the D - 1 last groups)
-    __syncwarp();
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const Coef<VC> o = coefficients<GIVEN, T, VC>(raw(d, 0, s), raw(d, 1, s), a);
-      ca[s] = o.a;
-      if (BACK) {
-        V hp = raw(d, 2, s).get();
-        if (ODD && time_of(now.i0 + s) == 0 && (in_now >> s & 1u)) hp = load_state<VC>(a.h0, now.b * (unsigned)a.H + now.u, now.n);
-        if (ODD && cut) hp = each(hp, [&](float x, int) { return (fresh_now >> s & 1u) ? 0.f : x; });
-        cb[s] = raw(d, 3, s).get();
-        slopes<GIVEN, VC>(o, hp, wg[BACK ? s : 0], wc[BACK ? s : 0]);
-      } else {
-        cb[s] = o.b;
-      }
-      if (ODD) {
-        const bool in = in_now >> s & 1u, fr = fresh_now >> s & 1u;
-        ca[s] = each(ca[s], [&](float x, int) { return !in ? 1.f : fr ? 0.f : x; });
-        cb[s] = each(cb[s], [&](float x, int) { return in ? x : 0.f; });
-      }
-    }
-    if (STAGED) __syncwarp();                  // the slot has been read
-    unsigned theirs = 0u;
-    if (a.deep) {
-      const Place later = place[(turn + D) % RING];
-      theirs = later.k >= 0 ? fetch(later, d) : none();
-    }
-
-    // one step of the scan: forward h -> a h + b, backward mu -> a (mu + seed)
-    const auto step = [&](int s, V h) {
-      if (ODD && cut) {                        // (a = 0 would not stop a NaN or an infinity)
-        const bool fr = fresh_now >> s & 1u;
-#pragma unroll
-        for (int v = 0; v < VC; ++v) h.at(v) = fr ? 0.f : h.at(v);
-        if (BACK) {
-          const V m = ca[s] * (h + cb[s]);
-          return each(m, [&](float x, int) { return fr ? 0.f : x; });
-        }
-      }
-      return BACK ? ca[s] * (h + cb[s]) : fma_(ca[s], h, cb[s]);
-    };
-    V A = V::all(1.f), h = V::all(0.f);
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      A = s == 0 ? ca[s] : ca[s] * A;
-      if (ODD && cut) A = each(A, [&](float x, int) { return (fresh_now >> s & 1u) ? 0.f : x; });
-      h = step(s, h);
-    }
-#pragma unroll
-    for (int v = 0; v < VC; ++v) pair[buf][warp][lane * VC + v] = make_float2(A.at(v), h.at(v));
-    if (threadIdx.x == 32 && a.deep) place[(turn + D + 1) % RING] = place_of(a, told, CT);
-    __syncthreads();                           // the only meeting of the block's warps: the arrays are used in turn
-
-    // every warp carries the state in front of the tile through the pairs of the warps before it; the last one speaks for the tile
-    const bool speaker = warp == kWarps - 1 && k + 1 < a.nk;
-    float2 whole[VC];
-    if (speaker) {
-#pragma unroll
-      for (int v = 0; v < VC; ++v) whole[v] = pair[buf][0][lane * VC + v];
-#pragma unroll
-      for (int w = 1; w < kWarps; ++w) {
-#pragma unroll
-        for (int v = 0; v < VC; ++v) whole[v] = through(pair[buf][w][lane * VC + v], whole[v], cut);
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < VC; ++v) h.at(v) = __uint_as_float(early[v]);
-    if (k > 0) {
-      bool known = true;
-#pragma unroll
-      for (int v = 0; v < VC; ++v) known = known && early[v] != kNone;
-      if (!__all_sync(0xffffffffu, known)) {
-        if (speaker) {
-#pragma unroll
-          for (int v = 0; v < VC; ++v) st_pair(a.pairs + word + v, whole[v]);
-        }
-        if (!NARROW || warp == kWarps - 1) {
-          h = look_back<VC, NARROW>(a, k, row, (i64)c * CT, lane);
-        } else {                               // the last warp asks L2 for all of them
-          uint64_t t0 = 0;
-          for (unsigned round = 0; posted[buf] != turn + 1u; ++round)
-            if ((round & 4095u) == 4095u && waited_too_long(a, lane, 31u, t0)) break;
-          __syncwarp();
-          __threadfence_block();
-          h = front[buf][lane];
-        }
-      }
-      if (NARROW && warp == kWarps - 1) {       // (whether it had to look back or not: the others asked a moment earlier)
-        front[buf][lane] = h;
-        __syncwarp();
-        __threadfence_block();
-        if (lane == 0) posted[buf] = turn + 1u;
-      }
-    }
-    if (speaker) {
-#pragma unroll
-      for (int v = 0; v < VC; ++v) st_word(a.states + word + v, word_of(through(whole[v], h.at(v), cut)));
-    }
-#pragma unroll
-    for (int w = 0; w < kWarps - 1; ++w) {
-#pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        const float2 p = pair[buf][w][lane * VC + v];
-        if (w < warp) h.at(v) = through(p, h.at(v), cut);
-      }
-    }
-    T *po = at(BACK ? a.dgate : a.h, now, time_of(now.i0)), *pw = BACK ? at(a.dcand, now, time_of(now.i0)) : nullptr;
-    const i64 dout = BACK ? -a.dgate.ts : a.h.ts;
-    const auto put = [&](T* p, const V& x) {
-      if constexpr (STAGED) {
-        store<T, VC>(p, x);
-      } else {
-#pragma unroll
-        for (int v = 0; v < VC; ++v)
-          if (v < now.n) p[v] = from_f32<T>(x.at(v));
-      }
-    };
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      V x, y;
-      if (BACK) {
-        const V lam = h + cb[s];
-        x = lam * wg[BACK ? s : 0];
-        y = lam * wc[BACK ? s : 0];
-      }
-      h = step(s, h);
-      if (!BACK) x = h;
-      bool write = true;
-      if (ODD) {
-        const int t = time_of(now.i0 + s);
-        write = now.n > 0 && t >= 0 && t < a.T;
-        const bool in = in_now >> s & 1u;
-        x = each(x, [&](float v, int) { return in ? v : 0.f; });
-        if (BACK) y = each(y, [&](float v, int) { return in ? v : 0.f; });
-      }
-      if (write) {
-        put(po + s * dout, x);
-        if (BACK) put(pw - s * a.dcand.ts, y);
-      }
-    }
-    float* last = BACK ? a.dh0 : a.hT;
-    if (last && k + 1 == a.nk && warp == kWarps - 1) store_state<VC>(last, now.b * (unsigned)a.H + now.u, h, now.n);
-    return theirs;
-  };
-  for (unsigned turn = 0, d = 0;; ++turn, d = d + 1 == D ? 0 : d + 1) {
-    if (!a.deep) {
-      if (threadIdx.x == 32) place[turn % RING] = place_of(a, draw(), CT);
-      __syncthreads();
-    }
-    const Place here = place[turn % RING];
-    if (here.k < 0) break;
-    const Spot now = spot_of(here, lane * VC);
-    if (!a.deep) {
-      ahead[0] = fetch(here, d);
-#pragma unroll
-      for (int i = 1; i < D; ++i) none();
-    }
-    const unsigned bits = ahead[0];
-    unsigned theirs;
-    if (__all_sync(0xffffffffu, bits == ALL && !(BACK && time_of(now.i0 + S - 1) <= 0)))
-      theirs = work(std::false_type{}, d, turn, here, now, bits & 0xffffu, bits >> 16);
-    else
-      theirs = work(std::true_type{}, d, turn, here, now, bits & 0xffffu, bits >> 16);
-#pragma unroll
-    for (int i = 0; i + 1 < D; ++i) ahead[i] = ahead[i + 1];
-    ahead[D - 1] = theirs;
-  }
-}
 
 // ---- arguments ---------------------------------------------------------------------------------------------------------------
 
@@ -710,20 +67,6 @@ int copy_state(float* dst, const float* src, size_t n, cudaStream_t s) {
   return e == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
 }
 
-constexpr int kWidest = 32 * 4;
-// Workspace: counter | states | pairs, filled with kNone.  Columns are padded to the wider column tile, time to the shortest one.
-constexpr int kLeastSteps = kStepsOf<false, true> * kWarps;
-static_assert(kLeastSteps <= kStepsOf<true, true> * kWarps && kLeastSteps <= kStepsOf<true, false> * kWarps && kLeastSteps <= kStepsOf<false, false> * kWarps,
-              "the shortest tile sizes the workspace");
-struct ScanSpace { size_t states, pairs, total; };
-ScanSpace scan_space(i64 nk, i64 padded) {
-  ScanSpace s;
-  s.states = 256;
-  s.pairs = s.states + (((size_t)nk * padded * sizeof(float) + 255) & ~(size_t)255);
-  s.total = s.pairs + (((size_t)nk * padded * sizeof(float2) + 255) & ~(size_t)255);
-  return s;
-}
-
 size_t scan_workspace(int T, int B, int H) {
   if (!scan_sizes_served(T, B, H) || T <= kLeastSteps || B == 0) return 0;
   return scan_space(((i64)T + kLeastSteps - 1) / kLeastSteps, ((i64)B * ((H + 3) / 4 * 4) + kWidest - 1) / kWidest * kWidest).total;
@@ -747,63 +90,6 @@ bool wide_columns(const ScanArgs& a, int dtype) {
   return a.H % n == 0 && fits(a.gate) && fits(a.cand) && fits(a.h) && fits(a.seed) && fits(a.dgate) && fits(a.dcand);
 }
 
-// blocks of a kernel that fit the device at once, asked once for each kernel and device
-template <class K> int resident_blocks(K kern, int threads, int smem, int (&known)[kMaxDevices]) {
-  const int dev = current_device_slot();
-  if (dev < 0) return 0;
-  if (!known[dev]) {
-    int per_sm = 0, sms = 0;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, smem) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-      return 0;
-    known[dev] = per_sm * sms;
-  }
-  return known[dev];
-}
-
-template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_scan(ScanArgs& a, void* ws, cudaStream_t s) {
-  constexpr int VC = kWide<T>;
-  if (a.T <= kShort) {
-    constexpr int VS = ALIGNED ? VC : 1;
-    const i64 cols = (i64)a.B * a.H;
-    scan_short_kernel<T, GIVEN, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
-  } else {
-    constexpr int steps = kStepsOf<ALIGNED, BACK> * kWarps, wide = 32 * VC;
-    a.Hp = (a.H + VC - 1) / VC * VC;
-    const i64 cols = (i64)a.B * a.Hp;
-    if (cols >= ((i64)1 << 31)) return MGRIT_UNSUPPORTED;
-    const i64 nc = (cols + wide - 1) / wide, nk = ((i64)a.T + steps - 1) / steps;
-    if (nk * nc >= INT32_MAX) return MGRIT_UNSUPPORTED;
-    a.nk = (int)nk; a.nc = (int)nc;
-    if (nk > 1) {
-      const ScanSpace sp = scan_space(nk, nc * wide);
-      char* w = static_cast<char*>(ws);
-      a.ticket = reinterpret_cast<unsigned*>(w);
-      a.states = reinterpret_cast<float*>(w + sp.states);
-      a.pairs = reinterpret_cast<unsigned long long*>(w + sp.pairs);
-      a.status = scan_status_ptr();
-      if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
-    }
-    // Few column tiles: every tile looks far back, and the blocks' warps in each other's way.  One warp then asks for all of them, for many
-    // pairs at a time (16384 steps of 2 x 64 units in bf16: 43 us against 62; 20000 of 1001: 133 against 151).  With more column tiles a
-    // state is usually there, and warps that look for themselves are ahead (4096 steps of 8 x 1024: 78 us against 92).
-    constexpr int smem = ALIGNED ? kAhead * (BACK ? 4 : 2) * kStepsOf<ALIGNED, BACK> * kWarps * 32 * 8 : 0;
-    const auto run = [&](auto kern, int (&known)[kMaxDevices]) {
-      const int most = resident_blocks(kern, kWarps * 32, smem, known);
-      if (most <= 0) { cudaGetLastError(); return false; }
-      // every block gets four tiles or more: enough that the first ones to run may take several at once
-      a.deep = nk * nc >= 4 * (i64)most;
-      kern<<<(unsigned)(nk * nc < most ? nk * nc : most), kWarps * 32, smem, s>>>(a);
-      return true;
-    };
-    static int known[2][kMaxDevices];
-    if (!(nc <= kNarrow ? run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, true>, known[0]) : run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, false>, known[1]))) return MGRIT_CUDA_ERROR;
-  }
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? MGRIT_OK : MGRIT_CUDA_ERROR;
-}
-
 int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cudaStream_t s) {
   ScanArgs a;
   int rc = check_scan(x, back, a);
@@ -813,15 +99,8 @@ int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cud
   if (need > 0 && (!ws || ((uintptr_t)ws & 255u))) return MGRIT_INVALID_ARG;
   if (ws_bytes < need) return MGRIT_WORKSPACE_TOO_SMALL;
   const bool wide = wide_columns(a, x->dtype), given = x->cell == MGRIT_SCAN_COEFFICIENTS;
-  with_elem(x->dtype, [&](auto tag) {
-    using T = decltype(tag);
-    const auto pick = [&](auto g) {
-      constexpr bool G = decltype(g)::value;
-      rc = wide ? (back ? launch_scan<T, G, true, true>(a, ws, s) : launch_scan<T, G, true, false>(a, ws, s))
-               : (back ? launch_scan<T, G, false, true>(a, ws, s) : launch_scan<T, G, false, false>(a, ws, s));
-    };
-    if (given) pick(std::true_type{}); else pick(std::false_type{});
-  });
+  if (need > 0 && !(a.status = scan_status_ptr())) return MGRIT_CUDA_ERROR;
+  with_elem(x->dtype, [&](auto tag) { rc = launch_scan<decltype(tag)>(a, wide, given, back, ws, s); });
   return rc;
 }
 

@@ -76,6 +76,14 @@ def test_many_columns():
     check_both(2, 3, 70001, F16, R.GIVEN, seed=2)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("T,B,H,lengths,reset", [(997, 24, 203, True, True), (1000, 100, 63, True, True), (1000, 60, 129, False, True), (1500, 7, 1001, True, False),
+                                                 (640, 64, 200, True, True), (700, 40, 202, False, False)])
+def test_many_tiles_of_odd_rows(T, B, H, lengths, reset, dtype):
+    """Rows at any address, tiles of one, two and more sequences, sequences that start and end anywhere, all blocks with several tiles."""
+    check_both(T, B, H, dtype, R.IMPLICIT, lengths=lengths, reset=reset, batch_major=H == 203, seed=H)
+
+
 @pytest.mark.parametrize("h0,seeds,dhT", [(False, True, True), (True, False, True), (False, True, False)])
 def test_absent_arrays(h0, seeds, dhT):
     check_both(150, 2, 24, F32, R.CLASSIC, h0=h0, seeds=seeds, dhT=dhT, seed=5)
