@@ -18,8 +18,8 @@
 //
 // Backward is the same scan from the last step to the first: mu_t = a_t (seed_t + mu_{t+1}).
 //
-// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 112 (61), backward 187 (123);
-// 65536 steps of 1024 units in fp32 forward 243 (123); one step of 32 x 1024 4.4.  What bounds it: two warps on each scheduler that issue
+// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 121 (61), backward 190 (123);
+// 65536 steps of 1024 units in fp32 forward 246 (123); one step of 32 x 1024 4.4.  What bounds it: two warps on each scheduler that issue
 // dependent arithmetic (42 % of the issue slots, exponentials and reciprocals 40 % of theirs, DRAM 39 %); with given coefficients the first
 // takes 80.  Few columns: the chain of tiles, 0.13 us each at 512 tiles.
 #pragma once
@@ -116,10 +116,11 @@ template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
 //   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2).
 // Small candidates take the first terms of the tangent's series, since G - 1 would lose their digits.  E stops at e^40 and G at e^20,
 // where z is 4e-18 and n is 1.
-// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, the series' first term for |c| < 2^-9 (left out: 1.3e-6 of the
-// value).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
+// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms of the series for |c| < 2^-4 (left out there: 2e-6 of
+// the value, as much as G - 1 has lost of it; one term for |c| < 2^-9: 112 us
+// for T 2048, B 32, H 1024 instead of 121, but 6e-5 of the value lost).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
 // bytes 61).  The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
-// coefficients are right to a few units in the last place; two terms of the series for |c| < 0.1 (left out: 5e-8).
+// coefficients are right to a few units in the last place; three terms of the series for |c| < 0.1 (left out: 5e-8).
 template <int VC> struct Coef { F<VC> a, b, q, n, e; };      // e = E / (K + E)
 template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
   constexpr bool FAST = sizeof(T) == 2;
@@ -140,7 +141,8 @@ template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coeff
   }
   o.n = (G + V::all(-1.0f)) * iq;
   if (FAST) {
-    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.001953125f ? c.at(i) : v; });
+    const V small = c * fma_(c * c, V::all(-0.33333334f), one);
+    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.0625f ? small.at(i) : v; });
   } else {
     const V c2 = c * c, small = c * fma_(c2, fma_(c2, V::all(0.13333334f), V::all(-0.33333334f)), one);
     o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.1f ? small.at(i) : v; });

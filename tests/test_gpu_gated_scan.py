@@ -77,7 +77,7 @@ def test_many_columns():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-@pytest.mark.parametrize("T,B,H,lengths,reset", [(997, 24, 203, True, True), (1000, 100, 63, True, True), (1000, 60, 129, False, True), (1500, 7, 1001, True, False),
+@pytest.mark.parametrize("T,B,H,lengths,reset", [(997, 24, 203, True, True), (1000, 100, 63, True, True), (1000, 60, 129, False, True), (300, 300, 17, True, True), (1500, 7, 1001, True, False),
                                                  (640, 64, 200, True, True), (700, 40, 202, False, False)])
 def test_many_tiles_of_odd_rows(T, B, H, lengths, reset, dtype):
     """Rows at any address, tiles of one, two and more sequences, sequences that start and end anywhere, all blocks with several tiles."""
