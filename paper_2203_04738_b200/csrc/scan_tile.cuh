@@ -116,10 +116,10 @@ template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
 //   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2).
 // Small candidates take the first terms of the tangent's series, since G - 1 would lose their digits.  E stops at e^40 and G at e^20,
 // where z is 4e-18 and n is 1.
-// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms of the series for |c| < 2^-4 (left out there: 2e-6 of
-// the value, as much as G - 1 has lost of it; one term for |c| < 2^-9: 112 us
-// for T 2048, B 32, H 1024 instead of 121, but 6e-5 of the value lost).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
-// bytes 61).  The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
+// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms of the series for |c| < 2^-4 (left out there: 2e-6 of the
+// value, as much as G - 1 has lost of it; one term for |c| < 2^-9 takes 112 us for T 2048, B 32, H 1024 instead of 121, but loses 6e-5).
+// Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the bytes 61).
+// The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
 // coefficients are right to a few units in the last place; three terms of the series for |c| < 0.1 (left out: 5e-8).
 template <int VC> struct Coef { F<VC> a, b, q, n, e; };      // e = E / (K + E)
 template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
