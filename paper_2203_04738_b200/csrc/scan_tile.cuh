@@ -59,7 +59,7 @@ template <bool BACK> constexpr int kStepsOf = BACK ? 8 : 16;
 constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2: 122 us for the 116 above)
 constexpr int kLook = 4;                       // looks of 32 tiles back
 constexpr int kFirst = 2, kMore = 16;          // pairs in flight in a look-back: of a column at first, of the thread's columns then
-constexpr int kNarrow = 8;                     // column tiles up to which one warp looks back for its block
+constexpr int kNarrow = 4;                     // column tiles up to which one warp looks back for its block
 constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
 constexpr float kMaxDt = 1e18f;
 
@@ -782,8 +782,9 @@ template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_kernels(ScanA
       if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
     }
     // Few column tiles: every tile looks far back, and the blocks' warps in each other's way.  One warp then asks for all of them, for many
-    // pairs at a time (16384 steps of 2 x 64 units in bf16: 43 us against 62; 20000 of 1001: 133 against 151).  With more column tiles a
-    // state is usually there, and warps that look for themselves are ahead (4096 steps of 8 x 1024: 78 us against 92).
+    // pairs at a time (16384 steps of 2 x 64 units in bf16, one column tile: 31 us against 60, backward 47 against 89).  With more column
+    // tiles a state is usually there, and warps that look for themselves are ahead (20000 steps of 1001, eight column tiles: 96 us against
+    // 99, backward 165 against 189; 4096 steps of 8 x 1024: 79 against 90).
     constexpr int smem = kAhead * (BACK ? 4 : 2) * kStepsOf<BACK> * kWarps * (ALIGNED ? 32 : 64) * 8;
     const auto run = [&](auto kern, int (&known)[kMaxDevices]) {
       const int most = resident_blocks(kern, kWarps * 32, smem, known);
