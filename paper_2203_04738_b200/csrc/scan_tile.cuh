@@ -226,7 +226,9 @@ __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArg
 // ---- words that tiles publish --------------------------------------------------------------------------------------------------
 
 constexpr unsigned kNone = 0xffffffffu;        // a NaN that no result is: NaN is published as 0x7fc00000
+constexpr unsigned kCut = 0x7fc00001u;         // in the place of a pair's A: a sequence starts in the piece, only B counts
 __device__ __forceinline__ unsigned word_of(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
+__device__ __forceinline__ bool is_cut(float2 p) { return __float_as_uint(p.x) == kCut; }
 __device__ __forceinline__ unsigned ld_word(const float* p) { unsigned v; asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v; }
 __device__ __forceinline__ void st_word(float* p, unsigned v) { asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" :: "l"(p), "r"(v) : "memory"); }
 __device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
@@ -235,14 +237,15 @@ __device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
 __device__ __forceinline__ void st_pair(unsigned long long* p, float2 v) {
-  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | word_of(v.x);
+  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | (is_cut(v) ? kCut : word_of(v.x));
   asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" :: "l"(p), "l"(w) : "memory");
 }
 __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t)); return t; }
 
-// h through the pair p.  cut (some sequence starts anew somewhere): A = 0 cuts off what came before, whatever it was (0 x NaN would not).
-__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && p.x == 0.f ? p.y : fmaf(p.x, h, p.y); }
-__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(cut && p.x == 0.f ? 0.f : p.x * q.x, through(p, q.y, cut)); }
+// h through the pair p.  cut (some sequence may start anew somewhere): kCut cuts off what came before, whatever it was (0 x NaN would not).  A
+// mark of its own, since a product of small coefficients is 0 as well, and a NaN goes on through those.
+__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && is_cut(p) ? p.y : fmaf(p.x, h, p.y); }
+__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(cut && (is_cut(p) || is_cut(q)) ? __uint_as_float(kCut) : p.x * q.x, through(p, q.y, cut)); }
 
 // One round of a wait, for the whole warp: true once it has run out, here or elsewhere (the status word says so).
 __device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, unsigned round, uint64_t& t0) {
@@ -608,9 +611,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       A = s == 0 ? ca[s] : ca[s] * A;
-      if (ODD && cut) A = each(A, [&](float x, int) { return (fresh_now >> s & 1u) ? 0.f : x; });
       h = step(s, h);
     }
+    if (ODD && cut && fresh_now != 0u) A = V::all(__uint_as_float(kCut));
 #pragma unroll
     for (int v = 0; v < VC; ++v) pair[buf][warp][lane * VC + v] = make_float2(A.at(v), h.at(v));
     if (threadIdx.x == 32 && a.deep) place[(turn + D + 1) % RING] = place_of(a, told, CT);
