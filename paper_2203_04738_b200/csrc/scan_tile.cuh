@@ -645,11 +645,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
         if (!NARROW || warp == kWarps - 1) {
           h = look_back<VC, NARROW, CUT>(a, k, row, (i64)c * CT, lane);
         } else {                               // the last warp asks L2 for all of them
-          // (the warp votes on what its lanes have read, so that they stay in the loop, or leave it, together)
+          // (every lane looks for itself, a bounded number of times; then the warp meets, and stays or leaves as one)
           uint64_t t0 = 0;
           bool there;
-          for (unsigned round = 0; !(there = __any_sync(0xffffffffu, posted[buf] == turn + 1u)); ++round)
-            if ((round & 4095u) == 4095u && waited_too_long(a, lane, 31u, t0)) break;
+          do {
+            unsigned round = 0;
+#pragma unroll 1
+            while (posted[buf] != turn + 1u && ++round < 4096u) {}
+            __syncwarp();
+            there = __any_sync(0xffffffffu, round < 4096u);
+          } while (!there && !waited_too_long(a, lane, 31u, t0));
           __syncwarp();
           __threadfence_block();
           h = there ? front[buf][lane] : V::all(__uint_as_float(0x7fc00000u));      // (run out: the results are void, and look it)
