@@ -2,5 +2,5 @@
 #include "scan_tile.cuh"
 
 namespace mg {
-template int launch_scan<float>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
+template int launch_scan<float>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
 }  // namespace mg

@@ -4,9 +4,9 @@
 
 namespace mg {
 
-extern template int launch_scan<float>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
-extern template int launch_scan<__nv_bfloat16>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
-extern template int launch_scan<__half>(ScanArgs&, bool, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<float>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
+extern template int launch_scan<__half>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
 
 namespace {
 
@@ -98,9 +98,10 @@ int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cud
   const size_t need = scan_workspace(a.T, a.B, a.H);
   if (need > 0 && (!ws || ((uintptr_t)ws & 255u))) return MGRIT_INVALID_ARG;
   if (ws_bytes < need) return MGRIT_WORKSPACE_TOO_SMALL;
-  const bool wide = wide_columns(a, x->dtype), given = x->cell == MGRIT_SCAN_COEFFICIENTS;
+  const bool wide = wide_columns(a, x->dtype);
+  const int mode = x->cell == MGRIT_SCAN_COEFFICIENTS ? kGiven : x->cell == MGRIT_CELL_CLASSIC && x->dt > 2.0f ? kLarge : kCells;
   if (need > 0 && !(a.status = scan_status_ptr())) return MGRIT_CUDA_ERROR;
-  with_elem(x->dtype, [&](auto tag) { rc = launch_scan<decltype(tag)>(a, wide, given, back, ws, s); });
+  with_elem(x->dtype, [&](auto tag) { rc = launch_scan<decltype(tag)>(a, wide, mode, back, ws, s); });
   return rc;
 }
 

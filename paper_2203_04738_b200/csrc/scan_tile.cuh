@@ -41,9 +41,11 @@ struct ScanArgs {
   unsigned* ticket; float* states; unsigned long long* pairs; int* status;      // [nk][nc * 32 VC] each
 };
 
+// Where coefficients come from: a cell, whose coefficients are at most 1 in size; the caller; the classic cell with dt > 2, up to dt - 1 in size
+enum { kCells = 0, kGiven = 1, kLarge = 2 };
 // Both directions for one element type (compiled in a file of its own).  wide: rows are made of whole aligned words of 16 bytes.  a.status
 // is set where the time axis may take more than one tile.
-template <class T> int launch_scan(ScanArgs& a, bool wide, bool given, bool back, void* ws, cudaStream_t s);
+template <class T> int launch_scan(ScanArgs& a, bool wide, int mode, bool back, void* ws, cudaStream_t s);
 
 namespace {
 
@@ -226,9 +228,7 @@ __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArg
 // ---- words that tiles publish --------------------------------------------------------------------------------------------------
 
 constexpr unsigned kNone = 0xffffffffu;        // a NaN that no result is: NaN is published as 0x7fc00000
-constexpr unsigned kCut = 0x7fc00001u;         // in the place of a pair's A: a sequence starts in the piece, only B counts
 __device__ __forceinline__ unsigned word_of(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
-__device__ __forceinline__ bool is_cut(float2 p) { return __float_as_uint(p.x) == kCut; }
 __device__ __forceinline__ unsigned ld_word(const float* p) { unsigned v; asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory"); return v; }
 __device__ __forceinline__ void st_word(float* p, unsigned v) { asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" :: "l"(p), "r"(v) : "memory"); }
 __device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
@@ -237,15 +237,31 @@ __device__ __forceinline__ float2 ld_pair(const unsigned long long* p) {
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
 __device__ __forceinline__ void st_pair(unsigned long long* p, float2 v) {
-  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | (is_cut(v) ? kCut : word_of(v.x));
+  const unsigned long long w = (unsigned long long)word_of(v.y) << 32 | word_of(v.x);
   asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" :: "l"(p), "l"(w) : "memory");
 }
 __device__ __forceinline__ uint64_t now_ns() { uint64_t t; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t)); return t; }
 
-// h through the pair p.  cut (some sequence may start anew somewhere): kCut cuts off what came before, whatever it was (0 x NaN would not).  A
-// mark of its own, since a product of small coefficients is 0 as well, and a NaN goes on through those.
-__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && is_cut(p) ? p.y : fmaf(p.x, h, p.y); }
-__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(cut && (is_cut(p) || is_cut(q)) ? __uint_as_float(kCut) : p.x * q.x, through(p, q.y, cut)); }
+// h through the pair p.  cut (some sequence may start anew somewhere): where one does, only B counts, whatever came before (0 x NaN would not cut
+// it off).  A = NaN says so, and stays that in products.  Nothing else that a NaN could say is lost: a gate of NaN makes B NaN too, and products
+// of given coefficients that are not finite are not handed on (below).  (A = 0 says less: small coefficients have such a product, and a NaN goes
+// on through those.)
+__device__ __forceinline__ float through(float2 p, float h, bool cut) { return cut && p.x != p.x ? p.y : fmaf(p.x, h, p.y); }
+__device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return make_float2(p.x * q.x, through(p, q.y, cut)); }
+
+// A product of coefficients says what becomes of a state of any size only as far as fp32 has room for it.
+//  * Coefficients of at most 1 in size: one that underflows is right to 2^-149 of the state.  It stays at the smallest number of its sign, so that
+//    an infinite state remains infinite.
+//  * Others (STRICT): an overflow, or digits lost below 2^-126 that coefficients above 1 may bring back, make it useless (3^128 times a state of
+//    zero is zero, inf times zero is NaN): kLost.  Such a piece is walked from its own first state instead.  Only the product of a whole tile whose
+//    coefficients are at most 1 may still underflow as above.  A zero among the coefficients makes it zero, whatever the others' product was.
+constexpr float kSteady = 1.001f;              // (roundings above 1 bring nothing back)
+constexpr float kLeast = 1.17549435e-38f, kMost = 3.4028235e38f;
+constexpr float kLost = INFINITY;              // in the place of a product (never published)
+__device__ __forceinline__ float kept(float p) { return p == 0.f ? copysignf(1.4e-45f, p) : p; }
+__device__ __forceinline__ float largest(float a, float b, float c) { float y; asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c)); return y; }      // in size; NaN is left out
+__device__ __forceinline__ float smallest_nan(float a, float b, float c) { float y; asm("min.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c)); return y; }      // in size; NaN stays
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
 // One round of a wait, for the whole warp: true once it has run out, here or elsewhere (the status word says so).
 __device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, unsigned round, uint64_t& t0) {
@@ -330,11 +346,12 @@ __device__ __forceinline__ Place place_of(const ScanArgs& a, unsigned tile, int 
 }
 
 // CUT: some sequence may start anew somewhere (a kernel of its own: decided at run time it costs those without starts 4 % backward)
-template <class T, bool GIVEN, bool ALIGNED, bool BACK, bool NARROW, bool CUT>
+template <class T, int MODE, bool ALIGNED, bool BACK, bool NARROW, bool CUT>
 __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_constant__ ScanArgs a) {
   constexpr int VC = kWide<T>, S = kStepsOf<BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
   extern __shared__ __align__(16) char stage[];      // [tiles ahead][warps][ARRAYS][S][32 threads, or 64 words] of 8 bytes
   constexpr unsigned ALL = (1u << S) - 1u;
+  constexpr bool GIVEN = MODE == kGiven, STRICT = MODE != kCells;
   using V = F<VC>;
   __shared__ __align__(16) float2 pair[2][kWarps][CT];
   constexpr int D = kAhead, RING = 4;
@@ -345,6 +362,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const i64 row = (i64)a.nc * CT;
   constexpr bool cut = CUT;
+  const bool starts_given = cut && (MODE != kLarge || a.reset.p);      // (kLarge has kernels with starts only)
   const auto time_of = [&](int i) { return BACK ? a.T - 1 - i : i; };
 
   // where the thread stands in a tile: sequence and unit of its columns, its first step counted from the scan's start
@@ -392,7 +410,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
   static_assert(S <= 16, "marks of two sequences in a warp");
   const auto paired = [&](const Spot& s) { return __shfl_sync(0xffffffffu, s.b, 31) - __shfl_sync(0xffffffffu, s.b, 0) <= 1u; };
   const auto marked = [&](const Known& x, const Spot& s) {
-    if (!cut || !paired(s)) return x.bits;
+    if (!starts_given || !paired(s)) return x.bits;
     const unsigned m = __ballot_sync(0xffffffffu, x.mark != 0u);
     return x.bits | (m >> ((s.b - __shfl_sync(0xffffffffu, s.b, 0)) * 16u) & x.bits & ALL) << 16;
   };
@@ -402,11 +420,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
     unsigned fresh = 0u, one = 0u;
     const int t0 = time_of(s.i0);
     const uint8_t* const marks = reinterpret_cast<const uint8_t*>(a.reset.p);
-    if (cut && paired(s)) {
+    if (starts_given && paired(s)) {
       const unsigned b = __shfl_sync(0xffffffffu, s.b, 0) + (lane >> 4);
       const int t = time_of(s.i0 + (lane & 15));
       if ((lane & 15) < S && b < (unsigned)a.B && t >= 0 && t < a.T) one = marks[(i64)t * a.reset.ts + (i64)b * a.reset.bs];
-    } else if (cut) {                          // all of them asked for before the first is looked at
+    } else if (starts_given) {                 // all of them asked for before the first is looked at
       uint8_t mark[S];
 #pragma unroll
       for (int i = 0; i < S; ++i) mark[i] = marks[(inside >> i & 1u) ? (i64)time_of(s.i0 + i) * a.reset.ts + (i64)s.b * a.reset.bs : 0];
@@ -613,24 +631,91 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
       A = s == 0 ? ca[s] : ca[s] * A;
       h = step(s, h);
     }
-    if (ODD && cut && fresh_now != 0u) A = V::all(__uint_as_float(kCut));
+    bool odd = false, lost = false;            // a coefficient above 1, or a product out of range; a column's product is not to be had
+    if (ODD && cut && fresh_now != 0u) {
+      A = V::all(__uint_as_float(0x7fc00000u));
+    } else if constexpr (STRICT) {
+      float most[2] = {0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int v = 0; v < VC; v += 2) most[s & 1] = largest(most[s & 1], ca[s].at(v), ca[s].at(v + 1 < VC ? v + 1 : v));
+      float least = A.at(0);
+#pragma unroll
+      for (int v = 0; v < VC; v += 2) least = smallest_nan(least, A.at(v), A.at(v + 1 < VC ? v + 1 : v));
+      if (!(fmaxf(most[0], most[1]) <= kSteady && least >= kLeast)) {
+        odd = true;
+        constexpr float kUp = S == 8 ? 32768.f : 128.f;      // S coefficients up to that, and down to its inverse, leave the product in range
+        static_assert(S == 8 || S == 16, "S powers of kUp are 2^120, or 2^112");
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+          float up = 0.f, down = kMost;
+#pragma unroll
+          for (int s = 0; s < S; ++s) { up = max_nan(up, fabsf(ca[s].at(v))); down = fminf(down, fabsf(ca[s].at(v))); }
+          if (up <= kMost && down == 0.f) A.at(v) = 0.f;
+          else if (!(up <= kSteady ? fabsf(A.at(v)) >= kLeast : up <= kUp && down * kUp >= 1.f)) A.at(v) = kLost, lost = true;
+        }
+      }
+    } else {
+      A = each(A, [](float x, int) { return kept(x); });
+    }
 #pragma unroll
     for (int v = 0; v < VC; ++v) pair[buf][warp][lane * VC + v] = make_float2(A.at(v), h.at(v));
     if (threadIdx.x == 32 && a.deep) place[(turn + D + 1) % RING] = place_of(a, told, CT);
-    __syncthreads();                           // the only meeting of the block's warps: the arrays are used in turn
+    // The only meeting of the block's warps, as a rule: the arrays are used in turn.  checks: some piece is odd; walk: some has to be walked.
+    bool checks = false, walk = false;
+    if constexpr (STRICT) {
+      checks = __syncthreads_or(odd);
+      if (checks) walk = __syncthreads_or(lost);
+    } else {
+      __syncthreads();
+    }
 
     // every warp carries the state in front of the tile through the pairs of the warps before it; the last one speaks for the tile
     const bool speaker = warp == kWarps - 1 && k + 1 < a.nk;
     float2 whole[VC];
-    if (speaker) {
+    const auto join = [&](bool cuts) {
 #pragma unroll
       for (int v = 0; v < VC; ++v) whole[v] = pair[buf][0][lane * VC + v];
 #pragma unroll
       for (int w = 1; w < kWarps; ++w) {
 #pragma unroll
-        for (int v = 0; v < VC; ++v) whole[v] = through(pair[buf][w][lane * VC + v], whole[v], cut);
+        for (int v = 0; v < VC; ++v) whole[v] = through(pair[buf][w][lane * VC + v], whole[v], cuts);
       }
-    }
+#pragma unroll
+      for (int v = 0; v < VC; ++v) {
+        float& p = whole[v].x;
+        if (!checks) {
+          p = kept(p);
+        } else if (p == p) {
+          float q = 1.f;
+          bool zero = false, out = false, large = false;
+#pragma unroll 1
+          for (int w = 0; w < kWarps; ++w) {
+            const float x = pair[buf][w][lane * VC + v].x;
+            zero = zero || x == 0.f;
+            large = large || fabsf(x) > kSteady;
+            q *= x;
+            out = out || !(fabsf(q) >= kLeast && fabsf(q) <= kMost);
+          }
+          p = zero ? 0.f : large && out ? kLost : kept(p);
+        }
+      }
+    };
+    // what the tile makes of the state in front of it; without a product: piece by piece
+    const auto tell = [&](const V& first, bool cuts) {
+#pragma unroll
+      for (int v = 0; v < VC; ++v) {
+        float x = through(whole[v], first.at(v), cuts);
+        if (STRICT && whole[v].x == kLost) {
+          x = first.at(v);
+#pragma unroll 1
+          for (int w = 0; w < kWarps; ++w) x = through(pair[buf][w][lane * VC + v], x, cuts);
+        }
+        st_word(a.states + word + v, word_of(x));
+      }
+    };
+    if (speaker && !walk) join(cut);
 #pragma unroll
     for (int v = 0; v < VC; ++v) h.at(v) = __uint_as_float(early[v]);
     if (k > 0) {
@@ -638,9 +723,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
 #pragma unroll
       for (int v = 0; v < VC; ++v) known = known && early[v] != kNone;
       if (!__all_sync(0xffffffffu, known)) {
-        if (speaker) {
+        if (speaker && !walk) {                // (a pair that does not come is waited for until the state behind it is there)
 #pragma unroll
-          for (int v = 0; v < VC; ++v) st_pair(a.pairs + word + v, whole[v]);
+          for (int v = 0; v < VC; ++v)
+            if (!STRICT || whole[v].x != kLost) st_pair(a.pairs + word + v, whole[v]);
         }
         if (!NARROW || warp == kWarps - 1) {
           h = look_back<VC, NARROW, CUT>(a, k, row, (i64)c * CT, lane);
@@ -667,16 +753,39 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
         if (lane == 0) posted[buf] = turn + 1u;
       }
     }
-    if (speaker) {
+    if (!walk) {
+      if (speaker) tell(h, cut);
 #pragma unroll
-      for (int v = 0; v < VC; ++v) st_word(a.states + word + v, word_of(through(whole[v], h.at(v), cut)));
-    }
+      for (int w = 0; w < kWarps - 1; ++w) {
 #pragma unroll
-    for (int w = 0; w < kWarps - 1; ++w) {
+        for (int v = 0; v < VC; ++v) {
+          const float2 p = pair[buf][w][lane * VC + v];
+          if (w < warp) h.at(v) = through(p, h.at(v), cut);
+        }
+      }
+    } else {
+      // One warp after the other: a column's piece without a product is walked, and what comes out of it takes the place of its pair.  Other
+      // columns go by their pairs as ever, so that their bits do not depend on their neighbours.
+      const V first = h;
+#pragma unroll 1
+      for (int w = 0; w < kWarps; ++w) {
+        if (w == warp && lost) {
+          V x = h;
 #pragma unroll
-      for (int v = 0; v < VC; ++v) {
-        const float2 p = pair[buf][w][lane * VC + v];
-        if (w < warp) h.at(v) = through(p, h.at(v), cut);
+          for (int s = 0; s < S; ++s) x = step(s, x);
+#pragma unroll
+          for (int v = 0; v < VC; ++v)
+            if (A.at(v) == kLost) pair[buf][w][lane * VC + v] = make_float2(__uint_as_float(0x7fc00000u), x.at(v));
+        }
+        __syncthreads();
+        if (w < warp) {
+#pragma unroll
+          for (int v = 0; v < VC; ++v) h.at(v) = through(pair[buf][w][lane * VC + v], h.at(v), true);
+        }
+      }
+      if (speaker) {
+        join(true);
+        tell(first, true);
       }
     }
     T *po = at(BACK ? a.dgate : a.h, now, time_of(now.i0)), *pw = BACK ? at(a.dcand, now, time_of(now.i0)) : nullptr;
@@ -769,12 +878,12 @@ template <class K> int resident_blocks(K kern, int threads, int smem, int (&know
   return known[dev];
 }
 
-template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_kernels(ScanArgs& a, void* ws, cudaStream_t s) {
+template <class T, int MODE, bool ALIGNED, bool BACK> int launch_kernels(ScanArgs& a, void* ws, cudaStream_t s) {
   constexpr int VC = kWide<T>;
   if (a.T <= kShort) {
     constexpr int VS = ALIGNED ? VC : 1;
     const i64 cols = (i64)a.B * a.H;
-    scan_short_kernel<T, GIVEN, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
+    scan_short_kernel<T, MODE == kGiven, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
   } else {
     constexpr int steps = kStepsOf<BACK> * kWarps, wide = 32 * VC;
     a.Hp = (a.H + VC - 1) / VC * VC;
@@ -805,8 +914,12 @@ template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_kernels(ScanA
       return true;
     };
     static int known[4][kMaxDevices];
-    const bool ok = nc <= kNarrow ? a.reset.p ? run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, true, true>, known[0]) : run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, true, false>, known[1])
-                    : a.reset.p ? run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, false, true>, known[2]) : run(scan_tile_kernel<T, GIVEN, ALIGNED, BACK, false, false>, known[3]);
+    bool ok;
+    if constexpr (MODE == kLarge)
+      ok = run(scan_tile_kernel<T, MODE, ALIGNED, BACK, false, true>, known[0]);
+    else
+      ok = nc <= kNarrow ? a.reset.p ? run(scan_tile_kernel<T, MODE, ALIGNED, BACK, true, true>, known[0]) : run(scan_tile_kernel<T, MODE, ALIGNED, BACK, true, false>, known[1])
+                         : a.reset.p ? run(scan_tile_kernel<T, MODE, ALIGNED, BACK, false, true>, known[2]) : run(scan_tile_kernel<T, MODE, ALIGNED, BACK, false, false>, known[3]);
     if (!ok) return MGRIT_CUDA_ERROR;
   }
   count_launch();
@@ -815,13 +928,18 @@ template <class T, bool GIVEN, bool ALIGNED, bool BACK> int launch_kernels(ScanA
 
 }  // namespace
 
-template <class T> int launch_scan(ScanArgs& a, bool wide, bool given, bool back, void* ws, cudaStream_t s) {
-  const auto pick = [&](auto g) {
-    constexpr bool G = decltype(g)::value;
-    return wide ? (back ? launch_kernels<T, G, true, true>(a, ws, s) : launch_kernels<T, G, true, false>(a, ws, s))
-                : (back ? launch_kernels<T, G, false, true>(a, ws, s) : launch_kernels<T, G, false, false>(a, ws, s));
+template <class T> int launch_scan(ScanArgs& a, bool wide, int mode, bool back, void* ws, cudaStream_t s) {
+  const auto pick = [&](auto m, auto w) {
+    constexpr int M = decltype(m)::value;
+    constexpr bool W = decltype(w)::value;
+    return back ? launch_kernels<T, M, W, true>(a, ws, s) : launch_kernels<T, M, W, false>(a, ws, s);
   };
-  return given ? pick(std::true_type{}) : pick(std::false_type{});
+  constexpr std::integral_constant<int, kCells> cells{};
+  constexpr std::integral_constant<int, kGiven> coefficients{};
+  // (states of the classic cell with dt > 2 grow without bound wherever its gates are open: one kernel for whatever is left)
+  if (mode == kLarge && a.T > kShort) return pick(std::integral_constant<int, kLarge>{}, std::false_type{});
+  if (mode == kGiven) return wide ? pick(coefficients, std::true_type{}) : pick(coefficients, std::false_type{});
+  return wide ? pick(cells, std::true_type{}) : pick(cells, std::false_type{});
 }
 
 }  // namespace mg
