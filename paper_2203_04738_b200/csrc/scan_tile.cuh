@@ -68,6 +68,8 @@ constexpr float kMaxDt = 1e18f;
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp_exact(float x) { const float y = rcp(x); return fmaf(fmaf(-x, y, 1.0f), y, y); }      // one Newton step
 
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
 // VC consecutive elements of a row, moved as one word
 template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
   T x[VC];
@@ -82,23 +84,19 @@ template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
     for (int i = 0; i < VC; ++i) x[i] = from_f32<T>(f.x[i]);
   }
 };
-// the same, no lower than -40 (gates) or no higher than 10 (candidates); NaN stays.  Two 16-bit values take one instruction.
-template <bool GATE> __device__ __forceinline__ float clamped(float v) { float y; if (GATE) asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(-40.f)); else asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(v), "f"(10.f)); return y; }
-template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; if (GATE) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc220c220u)); else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x41204120u)); return y; }
-template <bool GATE> __device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; if (GATE) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd100d100u)); else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0x49004900u)); return y; }
-template <bool GATE, class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Vec<T, VC>& x) {
+// the same, no lower than -40 (NaN stays).  Two 16-bit values take one instruction.
+__device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc220c220u)); return y; }
+__device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd100d100u)); return y; }
+template <class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Vec<T, VC>& x) {
   if constexpr (sizeof(T) == 2 && VC % 2 == 0) {
     Vec<T, VC> y;
     const unsigned* in = reinterpret_cast<const unsigned*>(&x);
     unsigned* out = reinterpret_cast<unsigned*>(&y);
 #pragma unroll
-    for (int i = 0; i < VC / 2; ++i) out[i] = clamped2<GATE>(in[i], T{});
+    for (int i = 0; i < VC / 2; ++i) out[i] = clamped2(in[i], T{});
     return y.get();
   } else {
-    F<VC> f = x.get();
-#pragma unroll
-    for (int i = 0; i < VC; ++i) f.x[i] = clamped<GATE>(f.x[i]);
-    return f;
+    return each(x.get(), [](float v, int) { return max_nan(v, -40.f); });
   }
 }
 template <class T, int VC> __device__ __forceinline__ Vec<T, VC> load(const T* p) { return *reinterpret_cast<const Vec<T, VC>*>(p); }
@@ -112,25 +110,23 @@ template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
   v.set(F<VC>::all(0.f));
   return v;
 }
-// The coefficients, and what their derivatives need.  With E = e^-g, G = e^2c and z = 1 / (1 + E):
-//   n = (G - 1) / (G + 1),  q = dt / (K + E),  a = 1 - q = (L + E) / (K + E),  b = q n
+// The coefficients, and what their derivatives need.  With E = e^-g, G = e^-2|c| and z = 1 / (1 + E):
+//   |n| = (1 - G) / (1 + G),  q = dt / (K + E),  a = 1 - q = (L + E) / (K + E),  b = q n
 // is the classic cell (q = dt z) for K = 1, L = 1 - dt and the implicit one (q = dt z / (1 + dt z)) for K = 1 + dt, L = 1, and in both
-//   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2).
-// Small candidates take the first terms of the tangent's series, since G - 1 would lose their digits.  E stops at e^40 and G at e^20,
-// where z is 4e-18 and n is 1.
-// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms of the series for |c| < 2^-4 (left out there: 2e-6 of the
-// value, as much as G - 1 has lost of it; one term for |c| < 2^-9 takes 112 us for T 2048, B 32, H 1024 instead of 121, but loses 6e-5).
-// Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the bytes 61).
-// The cost is two more roundings of fp32, far below those of the inputs.  fp32: one Newton step on each reciprocal, so that
-// coefficients are right to a few units in the last place; three terms of the series for |c| < 0.1 (left out: 5e-8).
-template <int VC> struct Coef { F<VC> a, b, q, n, e; };      // e = E / (K + E)
+//   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2),  1 - n^2 = 4 G / (1 + G)^2, which keeps its digits where |n| is near 1.
+// Small candidates take a polynomial, since 1 - G would lose their digits: tanh(c) / c = 1 + c^2 (..), coefficients by least squares on Chebyshev
+// points, weighted until the error is level.  E stops at e^40, where z is 4e-18.
+// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms for |c| < 0.1875 (error 9e-8 of n; n right to 6e-7 on either side
+// of the border).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
+// bytes 61).  The cost is two more roundings of fp32.  fp32: one Newton step on each reciprocal, three terms for |c| < 0.35 (4e-8, 4e-7).
+template <int VC> struct Coef { F<VC> a, b, q, n, e, m; };      // e = E / (K + E), m = 1 - n^2
 template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
   constexpr bool FAST = sizeof(T) == 2;
   Coef<VC> o;
   using V = F<VC>;
-  if (GIVEN) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = V::all(0.f); return o; }
-  const V one = V::all(1.0f), g = get_clamped<true>(graw), c = get_clamped<false>(craw);
-  const V E = each(g * V::all(-1.44269504f), [](float v, int) { return ex2(v); }), G = each(c * V::all(2.88539008f), [](float v, int) { return ex2(v); });
+  if (GIVEN) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = o.m = V::all(0.f); return o; }
+  const V one = V::all(1.0f), g = get_clamped(graw), c = craw.get();
+  const V E = each(g * V::all(-1.44269504f), [](float v, int) { return ex2(v); }), G = each(c * V::all(2.88539008f), [](float v, int) { return ex2(-fabsf(v)); });
   const V P = E + V::all(s.K), Q = G + one;
   V ip, iq;
   if (FAST) {
@@ -141,18 +137,16 @@ template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coeff
     ip = each(P, [](float v, int) { return rcp_exact(v); });
     iq = each(Q, [](float v, int) { return rcp_exact(v); });
   }
-  o.n = (G + V::all(-1.0f)) * iq;
-  if (FAST) {
-    const V small = c * fma_(c * c, V::all(-0.33333334f), one);
-    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.0625f ? small.at(i) : v; });
-  } else {
-    const V c2 = c * c, small = c * fma_(c2, fma_(c2, V::all(0.13333334f), V::all(-0.33333334f)), one);
-    o.n = each(o.n, [&](float v, int i) { return fabsf(c.at(i)) < 0.1f ? small.at(i) : v; });
-  }
+  const V far = fma_(G, V::all(-1.0f), one) * iq, c2 = c * c;
+  const V near = c * (FAST ? fma_(c2, fma_(c2, V::all(0.1307346f), V::all(-0.33330524f)), one)
+                           : fma_(c2, fma_(c2, fma_(c2, V::all(-0.04915929f), V::all(0.1330001f)), V::all(-0.3333267f)), one));
+  o.n = each(far, [&](float v, int i) { return fabsf(c.at(i)) < (FAST ? 0.1875f : 0.35f) ? near.at(i) : copysignf(v, c.at(i)); });
   o.q = ip * V::all(s.dt);
   o.a = FAST ? fma_(o.q, V::all(-1.0f), one) : (E + V::all(s.L)) * ip;
   o.b = o.q * o.n;
   o.e = E * ip;
+  const V w = iq + iq;
+  o.m = w * w * G;
   return o;
 }
 // d(gate), d(cand) of a step whose state has the derivative 1
@@ -160,7 +154,7 @@ template <bool GIVEN, int VC> __device__ __forceinline__ void slopes(const Coef<
   using V = F<VC>;
   if (GIVEN) { wg = hp; wc = V::all(1.0f); return; }
   wg = (k.q * k.e) * fma_(hp, V::all(-1.0f), k.n);
-  wc = k.q * (fma_(k.n, V::all(-1.0f), V::all(1.0f)) * (k.n + V::all(1.0f)));
+  wc = k.q * k.m;
 }
 
 // n of VC states (the others are zero, or not stored)
@@ -261,7 +255,6 @@ constexpr float kLost = INFINITY;              // in the place of a product (nev
 __device__ __forceinline__ float kept(float p) { return p == 0.f ? copysignf(1.4e-45f, p) : p; }
 __device__ __forceinline__ float largest(float a, float b, float c) { float y; asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c)); return y; }      // in size; NaN is left out
 __device__ __forceinline__ float smallest_nan(float a, float b, float c) { float y; asm("min.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c)); return y; }      // in size; NaN stays
-__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
 // One round of a wait, for the whole warp: true once it has run out, here or elsewhere (the status word says so).
 __device__ __forceinline__ bool waited_too_long(const ScanArgs& a, int lane, unsigned round, uint64_t& t0) {

@@ -193,3 +193,98 @@ def test_the_classic_cell_beyond_two(T, B, H, dtype):
         for what, x, r, bd in zip(("dgate", "dcand", "dh0"), got, refs, bounds):
             R.check(x, r, bd + (0 if what == "dh0" else R.rounding(r, dtype)), what)
     assert L.last_device_status() == 0
+
+
+# Saturated cells.  With E = e^-g the exponential's argument is rounded twice (2 u |g|) and it is off by two units in the last place itself (4 u):
+# E is off by (4 + 2.4 |g|) u of itself; a = (L + E) / (K + E) by that and 12 u for its sums, the reciprocal and the products, all in terms of
+# (|L| + E) / (K + E), which is a itself where 1 - dt is not negative; q = dt / (K + E) the same.  n by 64 u of itself.  1 - n^2 =
+# 4 G / (1 + G)^2 with G = e^-2|c| by (8 + 9.6 |c|) u and 8 u of itself.
+U = R.U
+
+
+def cell64(g, c, cell, dt):
+    K, L = (1 + dt, 1.0) if cell == R.IMPLICIT else (1.0, 1 - dt)
+    E, G = np.exp(-g), np.exp(-2 * np.abs(c))
+    a, pa, q, e = (L + E) / (K + E), (abs(L) + E) / (K + E), dt / (K + E), E / (K + E)
+    n, m = np.tanh(c), 4 * G / (1 + G) ** 2
+    kg, kc = (16 + 2.4 * np.abs(g)) * U, (16 + 9.6 * np.abs(c)) * U
+    return a, pa * kg, q, q * n, np.abs(q * n) * (kg + 64 * U), n, e, m, kg, kc
+
+
+def check_saturated(T, B, H, dtype, cell, dt, gates, cands, seed, seeds=False, h0=1.0):
+    from paper_2203_04738_b200 import binding as L
+    rng = np.random.default_rng(seed)
+    g, c = dev(rng.uniform(*gates, (T, B, H)), dtype), dev(rng.uniform(*cands, (T, B, H)), dtype)
+    s0, dT, sd = dev(h0 * rng.standard_normal((B, H))), dev(rng.standard_normal((B, H))), dev(rng.standard_normal((T, B, H)), dtype) if seeds else None
+    h, hT = L.gated_scan_forward(g, c, h0=s0, cell=cell, dt=dt)
+    a, da, q, b, db, n, e, m, kg, kc = cell64(R.to64(g), R.to64(c), cell, float(np.float32(dt)))
+    tiny = 2.0 ** -120                     # (products and exponentials below the normal numbers)
+    s = R.to64(s0)
+    S, err = np.abs(s), np.zeros((B, H))
+    ref, bound = np.zeros((T, B, H)), np.zeros((T, B, H))
+    for t in range(T):
+        err = np.abs(a[t]) * err + da[t] * (S + err) + db[t]
+        s, S = a[t] * s + b[t], np.abs(a[t]) * S + np.abs(b[t])
+        err += 2 * U * S + tiny
+        ref[t], bound[t] = s, err + 32 * U * S
+    R.check(h, ref, bound + R.rounding(ref, dtype), "h")
+    R.check(hT, ref[-1], bound[-1], "hT")
+    got = L.gated_scan_backward(g, c, h, h0=s0, dh_seed=sd, dhT=dT, cell=cell, dt=dt)
+    prev = np.concatenate((R.to64(s0)[None], R.to64(h)[:-1]))
+    mu = R.to64(dT)
+    S, err = np.abs(mu), np.zeros((B, H))
+    dg, dc, bg, bc = (np.zeros((T, B, H)) for _ in range(4))
+    for t in range(T - 1, -1, -1):
+        lam = mu + (0 if sd is None else R.to64(sd)[t])
+        S = S + (0 if sd is None else np.abs(R.to64(sd)[t]))
+        el = err + 34 * U * S
+        dg[t], dc[t] = lam * q[t] * e[t] * (n[t] - prev[t]), lam * q[t] * m[t]
+        bg[t] = q[t] * e[t] * (el * np.abs(n[t] - prev[t]) + (2 * kg[t] + 64 * U) * S * (np.abs(n[t]) + np.abs(prev[t]))) + tiny
+        bc[t] = q[t] * m[t] * (el + (kg[t] + kc[t] + 8 * U) * S) + tiny
+        err = np.abs(a[t]) * el + da[t] * (S + el)
+        mu, S = a[t] * lam, np.abs(a[t]) * S
+        err += 2 * U * S + tiny
+    for what, x, r, bd in zip(("dgate", "dcand", "dh0"), got, (dg, dc, mu), (bg, bc, err)):
+        R.check(x, r, bd + (0 if what == "dh0" else R.rounding(r, dtype)), what)
+    assert L.last_device_status() == 0
+
+
+RANGE = [(1, 3, 64), (3, 2, 33), (40, 2, 130), (300, 3, 33), (300, 5, 128)]
+CELL_DT = [(R.CLASSIC, 0.5), (R.CLASSIC, 1.0), (R.IMPLICIT, 1.0), (R.IMPLICIT, 4.0), (R.IMPLICIT, 64.0), (R.IMPLICIT, 1e4)]
+
+
+@pytest.mark.parametrize("T,B,H", RANGE)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cell,dt", CELL_DT[:3])
+def test_saturated_candidates_keep_the_digits_of_their_slope(T, B, H, dtype, cell, dt):
+    check_saturated(T, B, H, dtype, cell, dt, (-6, 1), (-30, 30), seed=T + H)
+    check_saturated(T, B, H, dtype, cell, dt, (-6, 1), (-30, 30), seed=T, seeds=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_infinite_candidates_are_candidates_of_one(dtype):
+    from paper_2203_04738_b200 import binding as L
+    T, B, H = 200, 2, 24
+    rng = np.random.default_rng(2)
+    gate, h0 = dev(rng.standard_normal((T, B, H)), dtype), dev(rng.standard_normal((B, H)))
+    sign = dev(np.where(rng.random((T, B, H)) < 0.5, -1.0, 1.0), dtype)
+    for cell in (R.CLASSIC, R.IMPLICIT):
+        far, near = (L.gated_scan_forward(gate, sign * x, h0=h0, cell=cell) for x in (float("inf"), 60.0))
+        assert torch.equal(far[0], near[0]) and torch.equal(far[1], near[1])
+        g = L.gated_scan_backward(gate, sign * float("inf"), far[0], h0=h0, dhT=h0, cell=cell)
+        assert not g[1].any() and torch.isfinite(g[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("T", [1, 20])
+def test_candidates_of_every_size(T, dtype):
+    """tanh itself, by b = n of one step (a gate of 100 leaves nothing else).  G = e^-2|c| is off by (4 + 4.8 |c|) u of itself, which 1 - G takes over
+    with its full size: at the border to the polynomial by 11 u of n in 16-bit types (|c| = 0.1875), by 6 u in fp32 (0.35).  The reciprocal and the
+    other roundings add 6 and 4 u, the reciprocal of the gate 4 u and 1 u, the last products 2 u.  The polynomial: 2 u and three roundings."""
+    from paper_2203_04738_b200 import binding as L
+    c = np.concatenate([s * np.geomspace(1e-4, 20, 20000) for s in (1, -1)]).reshape(1, 5, 8000)
+    cand = dev(np.repeat(c, T, 0), dtype)
+    n = np.tanh(R.to64(cand)[-1])
+    _, hT = L.gated_scan_forward(torch.full_like(cand, 100.0), cand, cell=R.CLASSIC)
+    err = np.abs(R.to64(hT) - n) / np.abs(n)
+    assert err.max() <= (13 if dtype == F32 else 23) * U, err.max() / U
