@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmgrit_gru.so")
 SOURCES = ["api.cu", "simt_kernels.cu", "f32_solve.cu", "stream_kernels.cu", "umma_engine.cu", "serial_kernels.cu", "scan_kernels.cu",
-           "scan_f32.cu", "scan_bf16.cu", "scan_f16.cu", "logit_kernels.cu"]
+           *(f"scan_{t}_{m}.cu" for t in ("f32", "bf16", "f16") for m in ("cells", "open", "given")), "logit_kernels.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC"]
 

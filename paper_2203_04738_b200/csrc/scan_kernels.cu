@@ -1,12 +1,21 @@
 // Gated linear recurrence: arguments, workspace, status word and entry points.  The kernels are in scan_tile.cuh, compiled for one element type
-// at a time.
+// and one origin of the coefficients at a time.
 #include "scan_tile.cuh"
 
 namespace mg {
 
-extern template int launch_scan<float>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
-extern template int launch_scan<__nv_bfloat16>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
-extern template int launch_scan<__half>(ScanArgs&, bool, int, bool, void*, cudaStream_t);
+extern template int launch_scan<float, kCells>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<float, kOpen>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<float, kGiven>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<float, kLarge>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16, kCells>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16, kOpen>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16, kGiven>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__nv_bfloat16, kLarge>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__half, kCells>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__half, kOpen>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__half, kGiven>(ScanArgs&, bool, bool, void*, cudaStream_t);
+extern template int launch_scan<__half, kLarge>(ScanArgs&, bool, bool, void*, cudaStream_t);
 
 namespace {
 
@@ -99,9 +108,17 @@ int run_scan(const gated_scan_args* x, bool back, void* ws, size_t ws_bytes, cud
   if (need > 0 && (!ws || ((uintptr_t)ws & 255u))) return MGRIT_INVALID_ARG;
   if (ws_bytes < need) return MGRIT_WORKSPACE_TOO_SMALL;
   const bool wide = wide_columns(a, x->dtype);
-  const int mode = x->cell == MGRIT_SCAN_COEFFICIENTS ? kGiven : x->cell == MGRIT_CELL_CLASSIC && x->dt > 2.0f ? kLarge : kCells;
+  const bool implicit = x->cell == MGRIT_CELL_IMPLICIT, walked = a.T <= kShort;
+  const int mode = x->cell == MGRIT_SCAN_COEFFICIENTS ? kGiven : !walked && x->dt <= (implicit ? 1.0f : 0.5f) ? kCells
+                   : !walked && !implicit && x->dt > 2.0f ? kLarge : kOpen;
   if (need > 0 && !(a.status = scan_status_ptr())) return MGRIT_CUDA_ERROR;
-  with_elem(x->dtype, [&](auto tag) { rc = launch_scan<decltype(tag)>(a, wide, mode, back, ws, s); });
+  with_elem(x->dtype, [&](auto tag) {
+    using T = decltype(tag);
+    rc = mode == kCells   ? launch_scan<T, kCells>(a, wide, back, ws, s)
+         : mode == kOpen  ? launch_scan<T, kOpen>(a, wide, back, ws, s)
+         : mode == kGiven ? launch_scan<T, kGiven>(a, wide, back, ws, s)
+                          : launch_scan<T, kLarge>(a, wide, back, ws, s);
+  });
   return rc;
 }
 

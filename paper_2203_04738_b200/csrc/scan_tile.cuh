@@ -41,11 +41,13 @@ struct ScanArgs {
   unsigned* ticket; float* states; unsigned long long* pairs; int* status;      // [nk][nc * 32 VC] each
 };
 
-// Where coefficients come from: a cell, whose coefficients are at most 1 in size; the caller; the classic cell with dt > 2, up to dt - 1 in size
-enum { kCells = 0, kGiven = 1, kLarge = 2 };
-// Both directions for one element type (compiled in a file of its own).  wide: rows are made of whole aligned words of 16 bytes.  a.status
-// is set where the time axis may take more than one tile.
-template <class T> int launch_scan(ScanArgs& a, bool wide, int mode, bool back, void* ws, cudaStream_t s);
+// Where coefficients come from: a cell with q <= 1/2 (implicit, dt <= 1; classic, dt <= 1/2); another one, whose coefficients are at most 1 in size;
+// the caller; the classic cell with dt > 2, up to dt - 1 in size.  (Kernels of their own for the first: without the choice of a that the others have
+// to make T 2048, B 32, H 1024 in bf16 takes 191 us backward for 199, with lengths and starts 194 forward for 210.)
+enum { kCells = 0, kOpen = 1, kGiven = 2, kLarge = 3 };
+// Both directions for one element type and origin of the coefficients (compiled in files of their own).  wide: rows are made of whole aligned words
+// of 16 bytes.  a.status is set where the time axis may take more than one tile.  Up to kShort steps: kOpen for every cell.
+template <class T, int MODE> int launch_scan(ScanArgs& a, bool wide, bool back, void* ws, cudaStream_t s);
 
 namespace {
 
@@ -115,16 +117,18 @@ template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
 // is the classic cell (q = dt z) for K = 1, L = 1 - dt and the implicit one (q = dt z / (1 + dt z)) for K = 1 + dt, L = 1, and in both
 //   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2),  1 - n^2 = 4 G / (1 + G)^2, which keeps its digits where |n| is near 1.
 // Small candidates take a polynomial, since 1 - G would lose their digits: tanh(c) / c = 1 + c^2 (..), coefficients by least squares on Chebyshev
-// points, weighted until the error is level.  E stops at e^40, where z is 4e-18.
-// FAST (16-bit types): both quotients from one reciprocal, a = 1 - q, two terms for |c| < 0.1875 (error 9e-8 of n; n right to 6e-7 on either side
+// points, weighted until the error is level.  a = 1 - q as long as that keeps its digits (a closed gate leaves the state as it is, to the last
+// bit, over any number of steps), the quotient from q = 1/2 on (where the gate is 15, 1 - q is off by tens of per cent).  E stops at e^40, where
+// z is 4e-18.
+// FAST (16-bit types): both quotients from one reciprocal, two terms for |c| < 0.1875 (error 9e-8 of n; n right to 6e-7 on either side
 // of the border).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
 // bytes 61).  The cost is two more roundings of fp32.  fp32: one Newton step on each reciprocal, three terms for |c| < 0.35 (4e-8, 4e-7).
 template <int VC> struct Coef { F<VC> a, b, q, n, e, m; };      // e = E / (K + E), m = 1 - n^2
-template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
+template <int MODE, class T, int VC> __device__ __forceinline__ Coef<VC> coefficients(const Vec<T, VC>& graw, const Vec<T, VC>& craw, const ScanArgs& s) {
   constexpr bool FAST = sizeof(T) == 2;
   Coef<VC> o;
   using V = F<VC>;
-  if (GIVEN) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = o.m = V::all(0.f); return o; }
+  if (MODE == kGiven) { o.a = graw.get(); o.b = craw.get(); o.q = o.n = o.e = o.m = V::all(0.f); return o; }
   const V one = V::all(1.0f), g = get_clamped(graw), c = craw.get();
   const V E = each(g * V::all(-1.44269504f), [](float v, int) { return ex2(v); }), G = each(c * V::all(2.88539008f), [](float v, int) { return ex2(-fabsf(v)); });
   const V P = E + V::all(s.K), Q = G + one;
@@ -142,7 +146,11 @@ template <bool GIVEN, class T, int VC> __device__ __forceinline__ Coef<VC> coeff
                            : fma_(c2, fma_(c2, fma_(c2, V::all(-0.04915929f), V::all(0.1330001f)), V::all(-0.3333267f)), one));
   o.n = each(far, [&](float v, int i) { return fabsf(c.at(i)) < (FAST ? 0.1875f : 0.35f) ? near.at(i) : copysignf(v, c.at(i)); });
   o.q = ip * V::all(s.dt);
-  o.a = FAST ? fma_(o.q, V::all(-1.0f), one) : (E + V::all(s.L)) * ip;
+  o.a = fma_(o.q, V::all(-1.0f), one);
+  if (MODE != kCells) {
+    const V part = (E + V::all(s.L)) * ip;
+    o.a = each(o.a, [&](float v, int i) { return o.q.at(i) < 0.5f ? v : part.at(i); });
+  }
   o.b = o.q * o.n;
   o.e = E * ip;
   const V w = iq + iq;
@@ -187,7 +195,7 @@ template <class T> struct Column {
   }
 };
 
-template <class T, bool GIVEN, int VC, bool BACK>
+template <class T, int MODE, int VC, bool BACK>
 __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArgs a) {
   using V = F<VC>;
   const Column<T> q(a, (blockIdx.x * kShortThreads + threadIdx.x) * VC);
@@ -201,12 +209,12 @@ __global__ void __launch_bounds__(kShortThreads) scan_short_kernel(const ScanArg
       continue;
     }
     const bool fresh = a.reset.p && q.fresh(a, t);
-    const Coef<VC> k = coefficients<GIVEN, T, VC>(load<T, VC>(q.at(a.gate, t)), load<T, VC>(q.at(a.cand, t)), a);
+    const Coef<VC> k = coefficients<MODE, T, VC>(load<T, VC>(q.at(a.gate, t)), load<T, VC>(q.at(a.cand, t)), a);
     if (BACK) {
       const V hp = fresh ? V::all(0.f) : t > 0 ? load<T, VC>(q.at(a.h, t - 1)).get() : load_state<VC>(a.h0, q.col);
       const V lam = a.seed.p ? h + load<T, VC>(q.at(a.seed, t)).get() : h;
       V wg, wc;
-      slopes<GIVEN, VC>(k, hp, wg, wc);
+      slopes<MODE == kGiven, VC>(k, hp, wg, wc);
       store<T, VC>(q.at(a.dgate, t), lam * wg);
       store<T, VC>(q.at(a.dcand, t), lam * wc);
       h = fresh ? V::all(0.f) : k.a * lam;
@@ -344,7 +352,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
   constexpr int VC = kWide<T>, S = kStepsOf<BACK>, CT = 32 * VC, SB = BACK ? S : 1, TT = S * kWarps, ARRAYS = BACK ? 4 : 2;
   extern __shared__ __align__(16) char stage[];      // [tiles ahead][warps][ARRAYS][S][32 threads, or 64 words] of 8 bytes
   constexpr unsigned ALL = (1u << S) - 1u;
-  constexpr bool GIVEN = MODE == kGiven, STRICT = MODE != kCells;
+  constexpr bool GIVEN = MODE == kGiven, STRICT = MODE == kGiven || MODE == kLarge;
   using V = F<VC>;
   __shared__ __align__(16) float2 pair[2][kWarps][CT];
   constexpr int D = kAhead, RING = 4;
@@ -573,7 +581,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
     if (!ODD || __any_sync(0xffffffffu, in_now != 0u)) {
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        const Coef<VC> o = coefficients<GIVEN, T, VC>(raw(0, s), raw(1, s), a);
+        const Coef<VC> o = coefficients<MODE, T, VC>(raw(0, s), raw(1, s), a);
         ca[s] = o.a;
         if (BACK) {
           V hp = raw(2, s).get();
@@ -586,7 +594,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
         }
         if (ODD) {
           const bool in = in_now >> s & 1u, fr = fresh_now >> s & 1u;
-          ca[s] = each(ca[s], [&](float x, int) { return !in ? 1.f : fr ? 0.f : x; });
+          // (a new sequence: step() takes the state for zero, which leaves a NaN among given coefficients to be kept out)
+          ca[s] = each(ca[s], [&](float x, int) { return !in ? 1.f : GIVEN && !BACK && fr ? 0.f : x; });
           cb[s] = each(cb[s], [&](float x, int) { return in ? x : 0.f; });
         }
       }
@@ -874,9 +883,11 @@ template <class K> int resident_blocks(K kern, int threads, int smem, int (&know
 template <class T, int MODE, bool ALIGNED, bool BACK> int launch_kernels(ScanArgs& a, void* ws, cudaStream_t s) {
   constexpr int VC = kWide<T>;
   if (a.T <= kShort) {
-    constexpr int VS = ALIGNED ? VC : 1;
-    const i64 cols = (i64)a.B * a.H;
-    scan_short_kernel<T, MODE == kGiven, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
+    if constexpr (MODE == kOpen || MODE == kGiven) {
+      constexpr int VS = ALIGNED ? VC : 1;
+      const i64 cols = (i64)a.B * a.H;
+      scan_short_kernel<T, MODE, VS, BACK><<<(unsigned)((cols / VS + kShortThreads - 1) / kShortThreads), kShortThreads, 0, s>>>(a);
+    }
   } else {
     constexpr int steps = kStepsOf<BACK> * kWarps, wide = 32 * VC;
     a.Hp = (a.H + VC - 1) / VC * VC;
@@ -921,18 +932,11 @@ template <class T, int MODE, bool ALIGNED, bool BACK> int launch_kernels(ScanArg
 
 }  // namespace
 
-template <class T> int launch_scan(ScanArgs& a, bool wide, int mode, bool back, void* ws, cudaStream_t s) {
-  const auto pick = [&](auto m, auto w) {
-    constexpr int M = decltype(m)::value;
-    constexpr bool W = decltype(w)::value;
-    return back ? launch_kernels<T, M, W, true>(a, ws, s) : launch_kernels<T, M, W, false>(a, ws, s);
-  };
-  constexpr std::integral_constant<int, kCells> cells{};
-  constexpr std::integral_constant<int, kGiven> coefficients{};
+template <class T, int MODE> int launch_scan(ScanArgs& a, bool wide, bool back, void* ws, cudaStream_t s) {
   // (states of the classic cell with dt > 2 grow without bound wherever its gates are open: one kernel for whatever is left)
-  if (mode == kLarge && a.T > kShort) return pick(std::integral_constant<int, kLarge>{}, std::false_type{});
-  if (mode == kGiven) return wide ? pick(coefficients, std::true_type{}) : pick(coefficients, std::false_type{});
-  return wide ? pick(cells, std::true_type{}) : pick(cells, std::false_type{});
+  if constexpr (MODE != kLarge)
+    if (wide) return back ? launch_kernels<T, MODE, true, true>(a, ws, s) : launch_kernels<T, MODE, true, false>(a, ws, s);
+  return back ? launch_kernels<T, MODE, false, true>(a, ws, s) : launch_kernels<T, MODE, false, false>(a, ws, s);
 }
 
 }  // namespace mg

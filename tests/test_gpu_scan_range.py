@@ -288,3 +288,33 @@ def test_candidates_of_every_size(T, dtype):
     _, hT = L.gated_scan_forward(torch.full_like(cand, 100.0), cand, cell=R.CLASSIC)
     err = np.abs(R.to64(hT) - n) / np.abs(n)
     assert err.max() <= (13 if dtype == F32 else 23) * U, err.max() / U
+
+
+@pytest.mark.parametrize("T,B,H", RANGE)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cell,dt", CELL_DT + [(R.IMPLICIT, 1e8)])
+def test_open_gates_keep_the_digits_of_what_they_leave(T, B, H, dtype, cell, dt):
+    """a is small where a gate is open or dt is large, and right to its own last digits: with the last state's derivative alone, every gradient is a
+    product of such coefficients."""
+    check_saturated(T, B, H, dtype, cell, dt, (-6, 30), (-30, 30), seed=T + H)
+    check_saturated(T, B, H, dtype, cell, dt, (6, 30), (-3, 3), seed=T, seeds=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_open_gates_of_steps_beyond_one(dtype):
+    """dt > 1 turns the classic cell's coefficient negative: a few steps of growing states, or dt = 2, whose coefficients are at most 1 in size."""
+    for T, dt in ((1, 64.0), (1, 1e4), (4, 64.0), (8, 4.0), (16, 2.0), (150, 2.0)):
+        check_saturated(T, 3, 40, dtype, R.CLASSIC, dt, (-6, 30), (-3, 3), seed=T)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_closed_gates_leave_a_state_as_it_is(dtype):
+    """z = e^-35 = 6e-16: a is 1, not a product of roundings near 1, over 20000 steps."""
+    from paper_2203_04738_b200 import binding as L
+    rng = np.random.default_rng(0)
+    h0 = dev(rng.uniform(0.5, 2.0, (1, 40)))
+    cand = dev(rng.standard_normal((20000, 1, 40)), dtype)
+    for cell in (R.CLASSIC, R.IMPLICIT):
+        h, hT = L.gated_scan_forward(torch.full_like(cand, -35.0), cand, h0=h0, cell=cell)
+        assert torch.equal(hT, h0)
+        assert torch.equal(L.gated_scan_backward(torch.full_like(cand, -35.0), cand, h, h0=h0, dhT=h0, cell=cell)[2], h0)
