@@ -289,6 +289,7 @@ typedef struct { void* data; int64_t t_stride, b_stride; } mgrit_rows;
  * stored h_t (not read behind a sequence's end); dhT[B,H] or NULL: w.r.t. the last state; one of the two must be given.
  *   Outputs: dgate, dcand (rows), dh0[B,H] or NULL.
  * A gate or candidate of NaN makes its step's state NaN (and the gradients of its step and of those before it).
+ * Gates below -86 count as -86 (z = 4.5e-38): a gate of -inf keeps the state at any dt.  Candidates of either infinity are candidates of 1 and -1.
  * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  B * H < 2^31, T < 2^31 - 1024, tiles of 64 steps x 32 units < 2^31. */
 typedef struct {
   int32_t T, B, H;

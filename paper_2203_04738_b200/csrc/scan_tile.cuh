@@ -86,9 +86,9 @@ template <class T, int VC> struct alignas(VC * sizeof(T)) Vec {
     for (int i = 0; i < VC; ++i) x[i] = from_f32<T>(f.x[i]);
   }
 };
-// the same, no lower than -40 (NaN stays).  Two 16-bit values take one instruction.
-__device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc220c220u)); return y; }
-__device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd100d100u)); return y; }
+// the same, no lower than -86 (NaN stays).  Two 16-bit values take one instruction.
+__device__ __forceinline__ unsigned clamped2(unsigned v, __nv_bfloat16) { unsigned y; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xc2acc2acu)); return y; }
+__device__ __forceinline__ unsigned clamped2(unsigned v, __half) { unsigned y; asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(y) : "r"(v), "r"(0xd560d560u)); return y; }
 template <class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Vec<T, VC>& x) {
   if constexpr (sizeof(T) == 2 && VC % 2 == 0) {
     Vec<T, VC> y;
@@ -98,7 +98,7 @@ template <class T, int VC> __device__ __forceinline__ F<VC> get_clamped(const Ve
     for (int i = 0; i < VC / 2; ++i) out[i] = clamped2(in[i], T{});
     return y.get();
   } else {
-    return each(x.get(), [](float v, int) { return max_nan(v, -40.f); });
+    return each(x.get(), [](float v, int) { return max_nan(v, -86.f); });
   }
 }
 template <class T, int VC> __device__ __forceinline__ Vec<T, VC> load(const T* p) { return *reinterpret_cast<const Vec<T, VC>*>(p); }
@@ -118,8 +118,8 @@ template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
 //   dh / dg = q E / (K + E) (n - h_prev),    dh / dc = q (1 - n^2),  1 - n^2 = 4 G / (1 + G)^2, which keeps its digits where |n| is near 1.
 // Small candidates take a polynomial, since 1 - G would lose their digits: tanh(c) / c = 1 + c^2 (..), coefficients by least squares on Chebyshev
 // points, weighted until the error is level.  a = 1 - q as long as that keeps its digits (a closed gate leaves the state as it is, to the last
-// bit, over any number of steps), the quotient from q = 1/2 on (where the gate is 15, 1 - q is off by tens of per cent).  E stops at e^40, where
-// z is 4e-18.
+// bit, over any number of steps), the quotient from q = 1/2 on (where the gate is 15, 1 - q is off by tens of per cent).  E stops at e^86:
+// z is 4.5e-38 then, so that a closed gate is one at the largest dt too, and (K + E) (1 + G) and its inverse are normal numbers.
 // FAST (16-bit types): both quotients from one reciprocal, two terms for |c| < 0.1875 (error 9e-8 of n; n right to 6e-7 on either side
 // of the border).  Four reciprocals and exponentials an element would take as long as its bytes (16 a cycle and SM: 65 us for 67 M elements, the
 // bytes 61).  The cost is two more roundings of fp32.  fp32: one Newton step on each reciprocal, three terms for |c| < 0.35 (4e-8, 4e-7).

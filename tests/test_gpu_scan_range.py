@@ -318,3 +318,29 @@ def test_closed_gates_leave_a_state_as_it_is(dtype):
         h, hT = L.gated_scan_forward(torch.full_like(cand, -35.0), cand, h0=h0, cell=cell)
         assert torch.equal(hT, h0)
         assert torch.equal(L.gated_scan_backward(torch.full_like(cand, -35.0), cand, h, h0=h0, dhT=h0, cell=cell)[2], h0)
+
+
+@pytest.mark.parametrize("T,B,H", RANGE)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cell,dt", CELL_DT + [(R.IMPLICIT, 1e12), (R.IMPLICIT, 1e18)])
+def test_closed_gates_stay_closed_at_any_dt(T, B, H, dtype, cell, dt):
+    check_saturated(T, B, H, dtype, cell, dt, (-84, -30), (-30, 30), seed=T + H, h0=1e-6)
+    check_saturated(T, B, H, dtype, cell, dt, (-84, 30), (-30, 30), seed=T, seeds=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("T", [1, 300])
+def test_a_gate_of_minus_infinity_keeps_the_state(T, dtype):
+    """z counts as e^-86 at least, 4.5e-38: even dt = 1e18 moves a state by no more than 4.5e-20 a step.  A gate of +inf is one of z = 1."""
+    from paper_2203_04738_b200 import binding as L
+    rng = np.random.default_rng(0)
+    h0, inf = dev(rng.uniform(0.5, 2.0, (2, 40))), float("inf")
+    cand = dev(rng.standard_normal((T, 2, 40)), dtype)
+    for cell in (R.CLASSIC, R.IMPLICIT):
+        for dt in (1.0, 1e18):
+            h, hT = L.gated_scan_forward(torch.full_like(cand, -inf), cand, h0=h0, cell=cell, dt=dt)
+            assert torch.equal(hT, h0)
+            g = L.gated_scan_backward(torch.full_like(cand, -inf), cand, h, h0=h0, dhT=h0, cell=cell, dt=dt)
+            assert torch.equal(g[2], h0) and g[1].abs().max().item() <= 1e-18
+        for a, b in zip(L.gated_scan_forward(torch.full_like(cand, inf), cand, h0=h0, cell=cell), L.gated_scan_forward(torch.full_like(cand, 120.0), cand, h0=h0, cell=cell)):
+            assert torch.equal(a, b) and torch.isfinite(a).all()
