@@ -536,8 +536,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
     const int k = here.k, c = here.c;
     const unsigned buf = turn & 1u;
     const i64 word = k * row + (i64)c * CT + lane * VC;
-    // The state in front: what the tile before has published, asked for early (it is usually there), or the first one, which every warp has
-    // read before the block meets, since the last tile may write its result over it (hT = h0).
+    // The state in front: what the tile before has published, asked for early (it is usually there), or the first one
     unsigned early[VC];
     if (k > 0) {
 #pragma unroll
@@ -664,6 +663,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
 #pragma unroll
     for (int v = 0; v < VC; ++v) pair[buf][warp][lane * VC + v] = make_float2(A.at(v), h.at(v));
     if (threadIdx.x == 32 && a.deep) place[(turn + D + 1) % RING] = place_of(a, told, CT);
+    if (k == 0) {
+      // The last tile may write its result over the first state (hT = h0), long after, but in another block, to which only the states that are
+      // published lead.  So every warp has its first state before the block meets, not just asked for it: what it does next depends on the values.
+      bool bad = false;
+#pragma unroll
+      for (int v = 0; v < VC; ++v) bad = bad || __uint_as_float(early[v]) != __uint_as_float(early[v]);
+      if (__any_sync(0xffffffffu, bad)) {
+#pragma unroll
+        for (int v = 0; v < VC; ++v) early[v] = word_of(__uint_as_float(early[v]));
+      }
+    }
     // The only meeting of the block's warps, as a rule: the arrays are used in turn.  checks: some piece is odd; walk: some has to be walked.
     bool checks = false, walk = false;
     if constexpr (STRICT) {
