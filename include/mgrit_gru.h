@@ -332,7 +332,7 @@ int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* log
  *   logits as above; top_id[N,K] (int32), top_logit[N,K]: the teacher's K best tokens of each row and their logits (or log
  *   probabilities: a constant of the row drops out), 1 <= K <= 1024.  With q = softmax(x / tau) over V and p = softmax(y / tau)
  *   over the row's K alternatives:   row_loss = tau^2 sum_k p_k (log p_k - log q[id_k]),   loss[1] = sum_r w_r row_loss_r,
- *   dlogits = w_r tau (q - p at the ids).   weight[N] or NULL: w_r, 1/N without it (the mean).
+ *   dlogits = w_r tau (q - p at the ids).   weight[N] or NULL: w_r, 1/N without it (the mean).   tau: 5e-39 .. 3e38.
  * An id outside [0, V) or a teacher logit of -inf is an absent alternative (p = 0); a row without any has loss 0 and gradient 0; an id
  * may occur twice, its probabilities then add up in the gradient.  A student logit of -inf has q = 0: where the teacher gives that token
  * a probability the loss is +inf and the gradient stays finite.  NaN, or +inf, of either side makes its row's loss and gradient NaN.

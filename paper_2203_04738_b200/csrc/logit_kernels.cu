@@ -671,7 +671,7 @@ struct DistillArgs {
   const int32_t* top_id; const float *top_logit, *weight; float *row_loss, *loss;
 };
 // The student's side of one row: q = 2^((x - m) c) / s with c = log2(e) / tau
-struct Student { float m, s; };
+struct Student { float m, s; };                // (differences first, then / tau: a logit / tau alone may leave the range, and loses digits)
 
 // f 2^((x - M) c) of the thread's vectors
 template <int G, class T> __device__ __forceinline__ void write_scaled(const Part<T>& p, int l, uint4* out, float M, float c, float f) {
@@ -698,7 +698,7 @@ template <int G, class T> __device__ __forceinline__ void write_scaled(const Par
 template <class T>
 __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits, T* dlogits, const DistillArgs a, int cluster) {
   constexpr int E = V16<T>::E, NW = kRow / 32;
-  extern __shared__ float teacher[];           // [K] logit / tau, then probability; [K] the student's logit; [K] token
+  extern __shared__ float teacher[];           // [K] logit, then probability; [K] the student's logit; [K] token
   float *prob = teacher, *gap = prob + a.K;
   int* id = reinterpret_cast<int*>(gap + a.K);
   __shared__ float wm[NW], wy[NW], wany[NW], wsum[NW], wmass[NW], wloss[NW];
@@ -717,7 +717,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
     const int v = a.top_id[(i64)r * a.K + k];
     const bool in = v >= 0 && v < a.V;
     id[k] = in ? v : -1;
-    prob[k] = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
+    prob[k] = in ? a.top_logit[(i64)r * a.K + k] : -INFINITY;
   }
   Seen t;
   Best unused;
@@ -741,7 +741,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
   const float m0 = ref_of(m), y0 = ref_of(ym);
   float s = warp_sum((t.s.x[0] + t.s.x[1]) * ex2((t.r - m0) * c)), mass = 0.f;
   if (teaches) {
-    for (int k = threadIdx.x; k < a.K; k += kRow) mass += ex2((prob[k] - y0) * kLog2e);
+    for (int k = threadIdx.x; k < a.K; k += kRow) mass += ex2((prob[k] - y0) * c);
     mass = warp_sum(mass);
   }
   if (lane == 0) { wsum[warp] = s; wmass[warp] = mass; }
@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
   if (teaches) {
     const float ls = logf(s), lmass = logf(all_sum<NW>(wmass));
     for (int k = threadIdx.x; k < a.K; k += kRow) {
-      const float logp = (prob[k] - y0) - lmass, pr = ex2(logp * kLog2e), z = gap[k];
+      const float logp = (prob[k] - y0) * inv - lmass, pr = ex2(logp * kLog2e), z = gap[k];
       const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
       loss += pr == 0.f ? 0.f : pr * (logp - logq);
       prob[k] = pr;
@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(kRow, kBlocks) distill_kernel(const T* logits,
   __syncthreads();
   if (rank == 0 && warp == NW - 1) {
     loss = all_sum<NW>(wloss);
-    if (lane == 0) a.row_loss[r] = present != 0.f ? a.tau * a.tau * loss : 0.f;
+    if (lane == 0) a.row_loss[r] = present != 0.f ? a.tau * (a.tau * loss) : 0.f;
   }
   if (!none && teaches) {
     const int begin = p.v0, stop = p.v0 + (int)p.n * E;      // the block's whole vectors
@@ -844,7 +844,7 @@ __global__ void __launch_bounds__(kWarpRows * 32, kBlocks) distill_warp_kernel(c
   for (int k = lane; k < a.K; k += 32) {
     const int v = a.top_id[(i64)r * a.K + k];
     const bool in = v >= 0 && v < a.V;
-    const float y = in ? a.top_logit[(i64)r * a.K + k] * inv : -INFINITY;
+    const float y = in ? a.top_logit[(i64)r * a.K + k] : -INFINITY;
     id[k] = in ? v : -1;
     prob[k] = y;
     gap[k] = in ? to_f32(row[v]) : -INFINITY;
@@ -862,18 +862,18 @@ __global__ void __launch_bounds__(kWarpRows * 32, kBlocks) distill_warp_kernel(c
   ym = warp_max(ym);
   any = __any_sync(0xffffffffu, any);
   const float y0 = ref_of(ym);
-  for (int k = lane; k < a.K; k += 32) mass += ex2((prob[k] - y0) * kLog2e);
+  for (int k = lane; k < a.K; k += 32) mass += ex2((prob[k] - y0) * c);
   mass = warp_sum(mass);
   const float ls = logf(s), lmass = logf(mass), gain = weight * a.tau;
   float loss = 0.f;
   for (int k = lane; k < a.K; k += 32) {
-    const float logp = (prob[k] - y0) - lmass, pr = ex2(logp * kLog2e), z = gap[k];
+    const float logp = (prob[k] - y0) * inv - lmass, pr = ex2(logp * kLog2e), z = gap[k];
     const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
     loss += pr == 0.f ? 0.f : pr * (logp - logq);
     prob[k] = pr;
   }
   loss = warp_sum(loss);
-  if (lane == 0) a.row_loss[r] = any ? a.tau * a.tau * loss : 0.f;
+  if (lane == 0) a.row_loss[r] = any ? a.tau * (a.tau * loss) : 0.f;
   const bool none = !any || weight == 0.f;
   const float f = s == 0.f ? 0.f : gain / s;
   const auto one = [&](float v) { return none ? 0.f : ex2((v - M) * c) * f; };
@@ -936,7 +936,7 @@ __global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* l
   s = group_sum<G>(s);
   const auto teacher = [&](int k) {
     const int v = k < a.K ? ids[k] : -1;
-    return v >= 0 && v < a.V ? ys[k] * inv : -INFINITY;
+    return v >= 0 && v < a.V ? ys[k] : -INFINITY;
   };
   float any = 0.f;
   for (int k = l; k < a.K; k += G) {
@@ -947,7 +947,7 @@ __global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* l
   ym = group_max<G>(ym);
   any = group_max<G>(any);
   const float y0 = ref_of(ym);
-  for (int k = l; k < a.K; k += G) mass += ex2((teacher(k) - y0) * kLog2e);
+  for (int k = l; k < a.K; k += G) mass += ex2((teacher(k) - y0) * c);
   mass = group_sum<G>(mass);
   const float ls = logf(s), lmass = logf(mass);
   float loss = 0.f;
@@ -957,7 +957,7 @@ __global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* l
     const bool in = v >= 0 && v < a.V;
     float p = 0.f;
     if (in) {
-      const float logp = (ys[k] * inv - y0) - lmass, z = to_f32(row[v]);
+      const float logp = (ys[k] - y0) * inv - lmass, z = to_f32(row[v]);
       const float logq = z == -INFINITY ? -INFINITY : (z - M) * inv - ls;
       p = ex2(logp * kLog2e);
       loss += p == 0.f ? 0.f : p * (logp - logq);
@@ -969,7 +969,7 @@ __global__ void __launch_bounds__(kShortThreads) distill_short_kernel(const T* l
     }
   }
   loss = group_sum<G>(loss);
-  loss = any != 0.f ? a.tau * a.tau * loss : 0.f;
+  loss = any != 0.f ? a.tau * (a.tau * loss) : 0.f;
   if (l == 0 && live) a.row_loss[r] = loss;
   const bool none = any == 0.f || weight == 0.f;
   const float scale = weight * a.tau, f = s == 0.f ? 0.f : 1.0f / s;
@@ -1108,7 +1108,7 @@ int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float t
   int rc = check_logits(N, V, dtype, logits, ld);
   if (rc == MGRIT_OK) rc = check_logits(N, V, dtype, dlogits, dld);
   if (rc != MGRIT_OK) return rc;
-  if (K < 1 || !(tau > 0.f) || tau > 3.0e38f || 1.0f / tau > 3.0e38f || !loss || !aligned4(loss)) return MGRIT_INVALID_ARG;
+  if (K < 1 || !(tau > 0.f) || tau > 3.0e38f || kLog2e / tau > 3.4e38f || !loss || !aligned4(loss)) return MGRIT_INVALID_ARG;
   if (K > kMaxTeacher || N > INT32_MAX / kMaxCluster) return MGRIT_UNSUPPORTED;
   cudaStream_t s = (cudaStream_t)stream;
   if (N > 0) {

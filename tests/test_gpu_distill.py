@@ -171,3 +171,37 @@ def test_results_repeat_and_replay():
                 o.zero_()
             g.replay()
             assert all(torch.equal(a, b) for a, b in zip(out, first))
+
+
+@pytest.mark.parametrize("V", [40, 300, 2500, 50000])
+@pytest.mark.parametrize("tau", [5e-39, 1e-38, 1e-30, 1e-3, 1e3, 1e18, 1e30])
+def test_temperatures_of_any_size(V, tau):
+    """A teacher's or student's distances are divided by tau, not their logits: a small tau names one token, a large one leaves the uniform
+    distribution."""
+    from paper_2203_04738_b200 import binding as L
+    for N in (5, 1300):
+        if N * V > 3e6:
+            continue
+        rng = np.random.default_rng(V)
+        K = 6
+        ids, y = teacher(N, V, K, V)
+        y += 100.0
+        x = rows(N, V, F32, V).clone()
+        ids[:, 0] = x.argmax(1).cpu().numpy()         # (the teacher's best is the student's)
+        w = np.full(N, 1.0, np.float32)
+        f = lambda a: torch.from_numpy(np.asarray(a, dtype=np.float32)).cuda()
+        loss, row, d = L.distill_topk_fwd_bwd(x, ints(ids), f(y), weight=f(w), temperature=tau)
+        t = float(np.float32(tau))
+        x64, y64 = R.to64(x), y.astype(np.float64)
+        q, p = np.exp(np.maximum((x64 - x64.max(1, keepdims=True)) / t, -1e4)), np.exp(np.maximum((y64 - y64.max(1, keepdims=True)) / t, -1e4))
+        q, p = q / q.sum(1, keepdims=True), p / p.sum(1, keepdims=True)
+        for r in range(N):
+            np.add.at(q[r], ids[r], -p[r])
+        assert torch.isfinite(d).all() and not row.isnan().any() and not loss.isnan().any()
+        if tau <= 1e18:                                   # (tau^2 times log(V / K) leaves fp32 beyond)
+            assert torch.isfinite(row).all() and (torch.isfinite(loss).all() or row.double().sum() > 3.4e38)      # (1300 rows of 2e36: 2.5e39)
+        # differences are exact to u of themselves, their exponents count to 150 at most: 2 (2 + 2.2 * 104) u and the sum's 40 u, of at most one each
+        far = np.abs(R.to64(d) / t - q)
+        assert far.max() <= 512 * R.U, far.max()
+        if tau <= 1e-30:
+            assert not row.any()

@@ -117,3 +117,8 @@ def test_a_sound_call_without_a_device_is_an_error_not_a_crash(L):
         pytest.skip("there is a device")
     assert logprob(L) == CUDA and logprob_back(L) == CUDA and distill(L) == CUDA
     assert L.lib.gated_scan_forward(scan_args(L), P, 1 << 30, None) == CUDA
+
+
+def test_distill_refuses_temperatures_whose_inverse_is_out_of_range(L):
+    for tau in (4e-39, 1e-44, 3.2e38):
+        assert distill(L, tau=tau) == INVALID, tau
