@@ -290,7 +290,10 @@ typedef struct { void* data; int64_t t_stride, b_stride; } mgrit_rows;
  *   Outputs: dgate, dcand (rows), dh0[B,H] or NULL.
  * A gate or candidate of NaN makes its step's state NaN (and the gradients of its step and of those before it).
  * Gates below -86 count as -86 (z = 4.5e-38): a gate of -inf keeps the state at any dt.  Candidates of either infinity are candidates of 1 and -1.
- * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  B * H < 2^31, T < 2^31 - 1024, tiles of 64 steps x 32 units < 2^31. */
+ * Coefficients of any size serve, also where their products leave the range of fp32 while no state does.  One limit: what 64 or more consecutive
+ * coefficients of at most 1 leave of a state is right to 2^-149 of that state, which later ones above 1 do not make better.
+ * T = 0 or B = 0 is an empty problem: hT = h0, dh0 = dhT.  T < 2^31 - 1024; B * H < 2^31, with H rounded up to a multiple of 4 (fp32: 2) for
+ * T > 8; tiles of 64 steps x 32 units < 2^31.  MGRIT_UNSUPPORTED beyond. */
 typedef struct {
   int32_t T, B, H;
   int32_t cell;                 /* MGRIT_CELL_CLASSIC, MGRIT_CELL_IMPLICIT or MGRIT_SCAN_COEFFICIENTS */
@@ -319,7 +322,7 @@ int gated_scan_backward(const gated_scan_args* args, void* ws, size_t ws_bytes, 
  * distribution: lse and all its log probabilities are -inf, its entropy 0.  A row with a NaN or +inf has NaN for all of its values
  * but the ids (NaN ranks behind -inf there).
  * token_logprobs_backward: dlogits_v = dlogprob ([v = token] - p_v) - dentropy p_v (log p_v + entropy), with p_v =
- *   exp(x_v - lse) from the given statistics (of the forward call); tokens and dlogprob, or entropy and dentropy, may be NULL
+ *   exp(x_v - lse) from the given statistics (of the forward call; N times the 16 KB pieces of a row < 2^31); tokens and dlogprob, or entropy and dentropy, may be NULL
  *   together, not all four; the token's term is absent for a token outside [0, V); where p_v is 0 so is its term; rows whose
  *   lse is -inf get zeros.  dlogits: N rows at dlogits + r * dld; it may be the logits array itself (same ld: in place). */
 int token_logprobs(int32_t N, int32_t V, int32_t dtype, const void* logits, int64_t ld, const int32_t* tokens, int32_t top,
@@ -335,7 +338,8 @@ int token_logprobs_backward(int32_t N, int32_t V, int32_t dtype, const void* log
  *   dlogits = w_r tau (q - p at the ids).   weight[N] or NULL: w_r, 1/N without it (the mean).   tau: 5e-39 .. 3e38.
  * An id outside [0, V) or a teacher logit of -inf is an absent alternative (p = 0); a row without any has loss 0 and gradient 0; an id
  * may occur twice, its probabilities then add up in the gradient.  A student logit of -inf has q = 0: where the teacher gives that token
- * a probability the loss is +inf and the gradient stays finite.  NaN, or +inf, of either side makes its row's loss and gradient NaN.
+ * a probability the loss is +inf and the gradient stays finite.  NaN, or +inf, of the student makes its row's loss and gradient NaN, of the
+ * teacher its row's loss and the gradient at all of the row's alternatives.
  * A row of weight zero has gradient zero whatever it holds, and adds nothing to loss.
  * row_loss[N] is required; sums run in a fixed order.  dlogits may be the logits array itself (same ld: in place). */
 int distill_topk_fwd_bwd(int32_t N, int32_t V, int32_t K, int32_t dtype, float tau, const void* logits, int64_t ld,

@@ -122,3 +122,14 @@ def test_a_sound_call_without_a_device_is_an_error_not_a_crash(L):
 def test_distill_refuses_temperatures_whose_inverse_is_out_of_range(L):
     for tau in (4e-39, 1e-44, 3.2e38):
         assert distill(L, tau=tau) == INVALID, tau
+
+
+def test_scan_refuses_columns_by_their_padded_width(L):
+    """More than 8 steps are taken by whole threads of columns, 4 of a 16-bit type or 2 of fp32."""
+    for kw in (dict(T=9, B=1 << 29, H=1, dtype=1), dict(T=9, B=1 << 29, H=3, dtype=2), dict(T=64, B=1 << 30, H=1, dtype=0), dict(T=9, B=(1 << 27) + 1, H=13, dtype=1)):
+        for fn in (L.lib.gated_scan_forward, L.lib.gated_scan_backward):
+            assert fn(scan_args(L, **kw), P, 1 << 62, None) == UNSUPPORTED, kw
+
+
+def test_gradients_of_more_pieces_than_a_grid_has_blocks_are_refused(L):
+    assert logprob_back(L, N=(1 << 27) - 1, V=1 << 20, ld=1 << 20, dld=1 << 20) == UNSUPPORTED
