@@ -376,6 +376,14 @@ def _require(ok, what, *args):
         raise ValueError(what.format(*args))
 
 
+def _int32(*sizes):
+    """Sizes as they are, refused beyond 32 bits (ctypes would cut them off)."""
+    for n in sizes:
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"a size of {n}: at most 2^31 - 1")
+    return sizes
+
+
 def _dtype(t):
     code = _DTYPES.get(t.dtype)
     _require(code is not None, "fp32, bf16 or fp16 required, got {}", t.dtype)
@@ -434,6 +442,13 @@ def _scan_head(gate, cand, h, reset, lengths, h0, cell, dt, shape, dev):
             0 if h0 is None else _like(h0, dev, shape[1:], torch.float32, "h0"), 0 if lengths is None else _like(lengths, dev, shape[1:2], torch.int32, "lengths"))
 
 
+def _scan_pack(*fields):
+    try:
+        return _SCAN_ARGS.pack(*fields)
+    except struct.error as e:
+        raise ValueError(f"a size or cell out of range: {e}") from None
+
+
 def _scan_call(fn, packed, shape, ws, dev):
     n = _scan_ws_bytes(*shape)
     if n == 0:
@@ -462,7 +477,7 @@ def gated_scan_forward(gate, cand, h0=None, cell=CELL_IMPLICIT, dt=1.0, lengths=
         last = hT.data_ptr()
     else:
         last = _like(hT, dev, shape[1:], torch.float32, "hT")
-    packed = _SCAN_ARGS.pack(*_scan_head(gate, cand, rows, reset, lengths, h0, cell, dt, shape, dev), last, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    packed = _scan_pack(*_scan_head(gate, cand, rows, reset, lengths, h0, cell, dt, shape, dev), last, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
     _scan_call(lib.gated_scan_forward, packed, shape, ws, dev)
     return h, hT
 
@@ -476,7 +491,7 @@ def gated_scan_backward(gate, cand, h, h0=None, dh_seed=None, dhT=None, cell=CEL
     dgate = gate.new_empty(shape) if dgate is None else dgate
     dcand = gate.new_empty(shape) if dcand is None else dcand
     dh0 = gate.new_empty(shape[1:], dtype=torch.float32) if dh0 is None else dh0
-    packed = _SCAN_ARGS.pack(*_scan_head(gate, cand, _strided(h, shape, t, dev, "h"), reset, lengths, h0, cell, dt, shape, dev), 0,
+    packed = _scan_pack(*_scan_head(gate, cand, _strided(h, shape, t, dev, "h"), reset, lengths, h0, cell, dt, shape, dev), 0,
                              *_strided(dh_seed, shape, t, dev, "dh_seed"), _like(dhT, dev, shape[1:], torch.float32, "dhT"),
                              *_strided(dgate, shape, t, dev, "dgate"), *_strided(dcand, shape, t, dev, "dcand"), _like(dh0, dev, shape[1:], torch.float32, "dh0"))
     _scan_call(lib.gated_scan_backward, packed, shape, ws, dev)
@@ -507,7 +522,7 @@ def token_logprobs(logits, tokens=None, top=0, out=None):
     -> TokenLogprobs of fp32 arrays (top_id int32).  `out`: a TokenLogprobs of an earlier call of the same sizes, to be overwritten."""
     p, ld = _logit_rows(logits, "logits")
     shape, dev, f32 = logits.shape, logits.device, torch.float32
-    N, V = shape
+    N, V, top = _int32(*shape, top)
     if out is None:
         each, ent, lse = logits.new_empty((3, N), dtype=f32).unbind()
         out = TokenLogprobs(None if tokens is None else each, ent, lse, logits.new_empty((N, top), dtype=f32) if top > 0 else None,
@@ -526,7 +541,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogprob=None, de
     """Gradient w.r.t. the logits, given those w.r.t. the tokens' log probabilities and / or the entropies and the statistics that the
     forward call returned.  dlogits may be the logits themselves (in place).  -> dlogits[N,V]"""
     p, ld = _logit_rows(logits, "logits")
-    (N, V), dev, f32 = logits.shape, logits.device, torch.float32
+    (N, V), dev, f32 = _int32(*logits.shape), logits.device, torch.float32
     rows = logits.shape[:1]
     dlogits = logits.new_empty((N, V)) if dlogits is None else dlogits
     d, dld = _logit_rows(dlogits, "dlogits", logits)
@@ -542,7 +557,7 @@ def distill_topk_fwd_bwd(logits, top_id, top_logit, weight=None, temperature=1.0
     dlogits may be the logits themselves (in place)."""
     p, ld = _logit_rows(logits, "logits")
     _require(top_id.dim() == 2, "top_id: matrix [N,K] required")
-    (N, V), K, dev, f32 = logits.shape, top_id.shape[1], logits.device, torch.float32
+    (N, V, K), dev, f32 = _int32(*logits.shape, top_id.shape[1]), logits.device, torch.float32
     rows = logits.shape[:1]
     if dlogits is None:
         dlogits = logits.new_empty((N, V))
