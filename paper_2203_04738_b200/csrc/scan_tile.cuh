@@ -63,7 +63,7 @@ template <bool BACK> constexpr int kStepsOf = BACK ? 8 : 16;
 constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2: 122 us for the 116 above)
 constexpr int kLook = 4;                       // looks of 32 tiles back
 constexpr int kFirst = 2, kMore = 16;          // pairs in flight in a look-back: of a column at first, of the thread's columns then
-constexpr int kNarrow = 4;                     // column tiles up to which one warp looks back for its block
+constexpr int kNarrow = 6;                     // column tiles up to which one warp looks back for its block (measured at the launch)
 constexpr uint64_t kWaitNs = 2000000000ull;    // bound of a look-back's wait
 constexpr float kMaxDt = 1e18f;
 
@@ -106,11 +106,6 @@ template <class T, int VC> __device__ __forceinline__ void store(T* p, F<VC> f) 
   Vec<T, VC> v;
   v.set(f);
   *reinterpret_cast<Vec<T, VC>*>(p) = v;
-}
-template <class T, int VC> __device__ __forceinline__ Vec<T, VC> zeros() {
-  Vec<T, VC> v;
-  v.set(F<VC>::all(0.f));
-  return v;
 }
 // The coefficients, and what their derivatives need.  With E = e^-g, G = e^-2|c| and z = 1 / (1 + E):
 //   |n| = (1 - G) / (1 + G),  q = dt / (K + E),  a = 1 - q = (L + E) / (K + E),  b = q n
@@ -915,9 +910,10 @@ template <class T, int MODE, bool ALIGNED, bool BACK> int launch_kernels(ScanArg
       if (!a.status || cudaMemsetAsync(ws, 0xff, sp.total, s) != cudaSuccess) { cudaGetLastError(); return MGRIT_CUDA_ERROR; }
     }
     // Few column tiles: every tile looks far back, and the blocks' warps in each other's way.  One warp then asks for all of them, for many
-    // pairs at a time (16384 steps of 2 x 64 units in bf16, one column tile: 31 us against 60, backward 47 against 89).  With more column
-    // tiles a state is usually there, and warps that look for themselves are ahead (20000 steps of 1001, eight column tiles: 96 us against
-    // 99, backward 165 against 189; 4096 steps of 8 x 1024: 79 against 90).
+    // pairs at a time.  With more column tiles a state is usually there, and warps that look for themselves are ahead.  16384 steps, us, one warp :
+    // every warp, for 1, 2, 4, 5, 6, 8 and 12 column tiles: bf16 forward 31 : 57, 32 : 53, 38 : 53, 45 : 60, 50 : 60, 63 : 69, 84 : 82, backward
+    // 48 : 90, 52 : 90, 72 : 105, 80 : 108, 90 : 115, 104 : 118, 139 : 141; fp32 forward 19 : 31, 21 : 32, 30 : 35, 35 : 39, 39 : 40, 50 : 48,
+    // 68 : 60, backward 29 : 53, 35 : 54, 51 : 63, 61 : 68, 71 : 71, 88 : 82, 119 : 103.
     constexpr int smem = kAhead * (BACK ? 4 : 2) * kStepsOf<BACK> * kWarps * (ALIGNED ? 32 : 64) * 8;
     const auto run = [&](auto kern, int (&known)[kMaxDevices]) {
       const int most = resident_blocks(kern, kWarps * 32, smem, known);
