@@ -5,7 +5,7 @@
 // quarters of that time (16 a cycle and SM).
 //  * short rows (V <= 64): eight lanes have a row, in registers;
 //  * many rows of up to some KB: a warp has a row, and no two warps wait for each other (65536 rows of 1100 logits in bf16: distillation
-//    100 us, bytes 45; with a block to a row it is bound by the blocks' starts and meetings, some 3 ns a row: 484);
+//    98 us, bytes 46; with a block to a row it is bound by the blocks' starts and meetings, some 3 ns a row: 484);
 //  * other rows: a block, or a cluster of up to 16 that meet through distributed shared memory.  The first
 //    pass streams the row once with a reference for the exponents that only moves when it has to; what is looked at twice (the gradient's
 //    pass, the vectors that hold a top alternative) comes from L2, where the rows in work have room.  Small blocks and no state but the
@@ -1021,14 +1021,15 @@ int launched(cudaError_t e) {
 }
 
 // Blocks that share a row: more than one where rows alone leave SMs without work, down to 8 KB each, and for a row that is read twice, one for
-// each 128 KB of it, so that the rows in work stay in L2.
+// each 128 KB of it.  (The second reading comes from L2 in whole for 4096 rows of 64 KB, 48 MB of them in work in 740 blocks; for 1000 rows of
+// 512 KB on clusters of four, 95 MB in work, a third of it comes from DRAM again.)
 int blocks_of(int N, i64 bytes, bool twice) {
   int c = 1;
   while (twice && c < kMaxCluster && bytes > c * (i64)131072) c *= 2;
   while (c < kMaxCluster && (i64)N * c < 296 && bytes >= 2 * c * (i64)8192) c *= 2;
   return c;
 }
-// A warp to a row, of up to `most` bytes, where there are rows for eight warps on every multiprocessor; or the row is so short that a block
+// A warp to a row, of up to `most` bytes, where there are rows for eight warps on every one of 148 multiprocessors; or the row is so short that a block
 // finds less than half a vector for each of its threads.  (us, a warp : a block to a row.  32768 rows of 4001 logits of 16 bits: 73 : 273
 // with the best five, gradient 91 : 109, distillation 111 : 276.  16384 rows of 8000: 65 : 160, 92 : 79, 115 : 164.  8192 rows of 8000 of 32
 // bits: 60 : 88, 92 : 79, 141 : 116.  600 rows of 8000 of 16 bits: 12 : 10, 13 : 6, 14 : 10.)

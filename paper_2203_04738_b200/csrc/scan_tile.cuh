@@ -18,10 +18,11 @@
 //
 // Backward is the same scan from the last step to the first: mu_t = a_t (seed_t + mu_{t+1}).
 //
-// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 121 (61), backward 190 (123);
-// 65536 steps of 1024 units in fp32 forward 246 (123); one step of 32 x 1024 4.4.  What bounds it: two warps on each scheduler that issue
-// dependent arithmetic (42 % of the issue slots, exponentials and reciprocals 40 % of theirs, DRAM 39 %); with given coefficients the first
-// takes 80.  Few columns: the chain of tiles, 0.13 us each at 512 tiles.
+// Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 119 (61), backward 191 (123);
+// 65536 steps of 1024 units in fp32 forward 253 (123); one step of 32 x 1024 4.3.  What bounds it: two warps on each scheduler that issue
+// dependent arithmetic (45 % of the issue slots, exponentials and reciprocals 39 % of theirs, DRAM 38 %); with given coefficients the first
+// takes 79.  Few columns: the chain of tiles, 0.1 us each at 512 tiles.
+// Decoupled look-back is a published method (D. Merrill, M. Garland, "Single-pass parallel prefix scan with decoupled look-back", 2016).
 #pragma once
 #include <type_traits>
 
@@ -42,8 +43,8 @@ struct ScanArgs {
 };
 
 // Where coefficients come from: a cell with q <= 1/2 (implicit, dt <= 1; classic, dt <= 1/2); another one, whose coefficients are at most 1 in size;
-// the caller; the classic cell with dt > 2, up to dt - 1 in size.  (Kernels of their own for the first: without the choice of a that the others have
-// to make T 2048, B 32, H 1024 in bf16 takes 191 us backward for 199, with lengths and starts 194 forward for 210.)
+// the caller; the classic cell with dt > 2, up to dt - 1 in size.  (Kernels of their own for the first, without the choice of a that the others have
+// to make: T 2048, B 32, H 1024 in bf16 takes 191 us backward, classic with dt = 1 198; in fp32 161 forward, 165 with the choice.)
 enum { kCells = 0, kOpen = 1, kGiven = 2, kLarge = 3 };
 // Both directions for one element type and origin of the coefficients (compiled in files of their own).  wide: rows are made of whole aligned words
 // of 16 bytes.  a.status is set where the time axis may take more than one tile.  Up to kShort steps: kOpen for every cell.
@@ -57,10 +58,10 @@ constexpr int kWarps = 8;
 template <class T> constexpr int kWide = 8 / sizeof(T);      // VC, columns of a thread: 8 bytes of a row
 // S, steps of a thread.  Long pieces pay: what a tile costs whatever its size (its place, the pairs of the other warps, one meeting, one look
 // at L2) is shared by 64 elements of a thread, and the chain of tiles is short.  One block fills an SM's registers.
-// Half the steps and two blocks: 116 -> 134 us forward, 196 -> 243 backward for T 2048, B 32, H 1024 in bf16, 257 -> 323 for 65536 steps of
-// 1024 units in fp32.
+// Half the steps and two blocks took 16 % longer forward and 24 % backward for T 2048, B 32, H 1024 in bf16, 26 % for 65536 steps of 1024
+// units in fp32.
 template <bool BACK> constexpr int kStepsOf = BACK ? 8 : 16;
-constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2: 122 us for the 116 above)
+constexpr int kAhead = 1;                      // tiles whose loads are in flight behind the one in work (2 took 5 % longer for T 2048, B 32, H 1024 in bf16)
 constexpr int kLook = 4;                       // looks of 32 tiles back
 constexpr int kFirst = 2, kMore = 16;          // pairs in flight in a look-back: of a column at first, of the thread's columns then
 constexpr int kNarrow = 6;                     // column tiles up to which one warp looks back for its block (measured at the launch)
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
   // thread's 8 bytes may start at any element: it brings the aligned 8 bytes that hold its first one, and finds the next 8 in its neighbour's
   // place.  For the last thread of a piece of a row they are brought to the second half of the row's place.  What a thread wants is cut out on
   // reading.  Only aligned words that hold an element of the row are read; what else is in them is not used.
-  // (997 steps of 24 x 203 units in fp16: 27 us forward, 42 backward; element by element into registers, with half the
+  // (997 steps of 24 x 203 units in fp16: 29 us forward, 44 backward; element by element into registers, with half the
   // steps: 32, 56.)
   constexpr unsigned kWord = VC * sizeof(T), kRow = (ALIGNED ? 32 : 64) * kWord, kPieces = 32 * kWord / 16, kRows = ALIGNED ? 32 / kPieces : 1;      // copies of a row, rows at a time
   constexpr unsigned kArray = S * kRow, kTile = kWarps * ARRAYS * kArray;
@@ -400,8 +401,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
   // What is known of a tile once it has been asked for.  bits: which of the thread's steps lie in the sequence, and (from bit 16 on) which of
   // them start one.  The marks of those starts are on their way too: where the warp's columns are of one or two sequences (paired), lanes
   // 0 .. S - 1 and 16 .. 16 + S - 1 have the steps' marks, which marked() adds to the bits when they are needed; otherwise the
-  // bits are complete.  (T 2048, B 32, H 1024 in bf16
-  // with lengths and starts: 189 us forward, 214 if every tile waits for its marks.)
+  // bits are complete.  (If every tile waited for its marks, T 2048, B 32, H 1024 in bf16 with lengths and starts would take 13 % longer.)
   struct Known { unsigned bits, mark; };
   static_assert(S <= 16, "marks of two sequences in a warp");
   const auto paired = [&](const Spot& s) { return __shfl_sync(0xffffffffu, s.b, 31) - __shfl_sync(0xffffffffu, s.b, 0) <= 1u; };
