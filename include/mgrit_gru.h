@@ -288,7 +288,8 @@ typedef struct { void* data; int64_t t_stride, b_stride; } mgrit_rows;
  * Backward, at the GIVEN states h (what the forward call stored): dh_seed (rows) or data == NULL: loss derivative w.r.t. each
  * stored h_t (not read behind a sequence's end); dhT[B,H] or NULL: w.r.t. the last state; one of the two must be given.
  *   Outputs: dgate, dcand (rows), dh0[B,H] or NULL.
- * A gate or candidate of NaN makes its step's state NaN (and the gradients of its step and of those before it).
+ * A gate of NaN makes its step's state NaN, and the gradients of its step and of those before it; a candidate of NaN its step's state and
+ * gradients, and with a cell in a 16-bit type (whose two quotients have one reciprocal) those of the steps before it too.
  * Gates below -86 count as -86 (z = 4.5e-38): a gate of -inf keeps the state at any dt.  Candidates of either infinity are candidates of 1 and -1.
  * Coefficients of any size serve, also where their products leave the range of fp32 while no state does.  One limit: what 64 or more consecutive
  * coefficients of at most 1 leave of a state is right to 2^-149 of that state, which later ones above 1 do not make better.

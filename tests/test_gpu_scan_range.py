@@ -344,3 +344,46 @@ def test_a_gate_of_minus_infinity_keeps_the_state(T, dtype):
             assert torch.equal(g[2], h0) and g[1].abs().max().item() <= 1e-18
         for a, b in zip(L.gated_scan_forward(torch.full_like(cand, inf), cand, h0=h0, cell=cell), L.gated_scan_forward(torch.full_like(cand, 120.0), cand, h0=h0, cell=cell)):
             assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cell,dt", [(R.CLASSIC, 0.5), (R.CLASSIC, 1.0), (R.IMPLICIT, 1.0), (R.IMPLICIT, 8.0), (R.GIVEN, 1.0)])
+@pytest.mark.parametrize("T,B,H", [(7, 3, 40), (150, 2, 24), (520, 6, 33), (700, 3, 512)])
+def test_scattered_values_that_are_not_finite(T, B, H, cell, dt, dtype):
+    """NaN in every input, infinities among states and derivatives: they reach what the definition says they reach, whatever starts and ends around
+    them, and everything else is right."""
+    from paper_2203_04738_b200 import binding as L
+    nan, inf = float("nan"), float("inf")
+    for seed, (lengths, reset) in enumerate(((False, False), (True, False), (False, True), (True, True))):
+        rng = np.random.default_rng(100 * seed + T)
+
+        def made(x, values, share):
+            x = np.clip(x, -4, 4)
+            for v in values:
+                x = np.where(rng.random(x.shape) < share / len(values), v, x)
+            return x
+
+        few = 3 / (T * B * H) if T * B * H > 3000 else 0.003
+        gate = made(rng.standard_normal((T, B, H)) - (0 if cell == R.GIVEN else 1), (nan,), few)
+        if cell == R.GIVEN:
+            gate = gate / 5
+        arrays = dict(g=dev(gate, dtype), c=dev(made(rng.standard_normal((T, B, H)), (nan,), few), dtype), h0=dev(made(rng.standard_normal((B, H)), (nan, inf, -inf), 0.1)),
+                      hs=dev(made(rng.standard_normal((T, B, H)), (nan,), few), dtype), sd=dev(made(rng.standard_normal((T, B, H)), (nan, inf, -inf), 3 * few), dtype),
+                      dT=dev(made(rng.standard_normal((B, H)), (nan, inf, -inf), 0.1)))
+        ln = rng.integers(0, T + 1, B).astype(np.int32) if lengths else None
+        rs = (rng.random((T, B)) < 4 / T).astype(np.uint8) if reset else None
+        kw = dict(cell=cell, dt=dt, lengths=None if ln is None else dev(ln, torch.int32), reset=None if rs is None else dev(rs, torch.uint8))
+        n = {k: R.to64(v) for k, v in arrays.items()}
+        clean = lambda x: np.nan_to_num(x, nan=0, posinf=0, neginf=0)
+        h, hT = L.gated_scan_forward(arrays["g"], arrays["c"], h0=arrays["h0"], **kw)
+        with np.errstate(invalid="ignore", over="ignore"):
+            ref, refT, bound, boundT = R.scan_forward(n["g"], n["c"], n["h0"], cell, dt, ln, rs)
+            # (a candidate of NaN in a 16-bit type reaches the steps before it in the backward pass, as a gate of NaN does)
+            g64 = np.where(np.isnan(n["c"]), nan, n["g"]) if dtype != F32 and cell != R.GIVEN else n["g"]
+            refs, bounds = R.scan_backward(g64, n["c"], n["hs"], n["h0"], n["sd"], n["dT"], cell, dt, ln, rs)
+        R.check(h, ref, clean(bound) + R.rounding(clean(ref), dtype), "h")
+        R.check(hT, refT, clean(boundT), "hT")
+        got = L.gated_scan_backward(arrays["g"], arrays["c"], arrays["hs"], h0=arrays["h0"], dh_seed=arrays["sd"], dhT=arrays["dT"], **kw)
+        for what, x, r, bd in zip(("dgate", "dcand", "dh0"), got, refs, bounds):
+            R.check(x, r, clean(bd) + (0 if what == "dh0" else R.rounding(clean(r), dtype)), what)
+    assert L.last_device_status() == 0
