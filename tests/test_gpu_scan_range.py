@@ -387,3 +387,35 @@ def test_scattered_values_that_are_not_finite(T, B, H, cell, dt, dtype):
         for what, x, r, bd in zip(("dgate", "dcand", "dh0"), got, refs, bounds):
             R.check(x, r, clean(bd) + (0 if what == "dh0" else R.rounding(clean(r), dtype)), what)
     assert L.last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,B,H,batch_major", [(90, 2, 24, False), (150, 3, 33, True), (520, 2, 64, False), (700, 2, 520, False), (700, 5, 121, True)])
+@pytest.mark.parametrize("span", [3, 20, 60])
+def test_coefficients_of_any_size_between_bounded_states(span, T, B, H, batch_major, dtype):
+    """States that jump between levels 2^-span .. 2^span at every step, by coefficients of up to 2^(2 span) in size, some of them zero."""
+    from paper_2203_04738_b200 import binding as L
+    for seed, (lengths, reset) in enumerate(((False, False), (True, False), (False, True), (True, True))):
+        rng = np.random.default_rng(10 * T + seed)
+        level = rng.integers(-span, span + 1, (T + 1, B, H)).astype(np.float64)
+        a = 2.0 ** (level[1:] - level[:-1]) * np.where(rng.random((T, B, H)) < 0.5, -1, 1) * (rng.random((T, B, H)) > 0.01)
+        arr = (lambda x: x.transpose(0, 1)) if batch_major else (lambda x: x)
+        lay = lambda x: arr(dev(x.swapaxes(0, 1) if batch_major else x, dtype))
+        n = lambda *s: rng.standard_normal(s)
+        g, c, hs, sd = lay(a), lay(2.0 ** level[1:] * n(T, B, H)), lay(2.0 ** level[1:] * n(T, B, H)), lay(2.0 ** -level[1:] * n(T, B, H))
+        h0 = dev(2.0 ** level[0] * n(B, H))
+        ln = rng.integers(0, T + 1, B).astype(np.int32) if lengths else None
+        rs = (rng.random((T, B)) < 4 / T).astype(np.uint8) if reset else None
+        end = np.full(B, T) if ln is None else ln
+        dT = dev(2.0 ** -np.take_along_axis(level, end[None, :, None], 0)[0] * n(B, H))
+        kw = dict(cell=R.GIVEN, h0=h0, lengths=None if ln is None else dev(ln, torch.int32), reset=None if rs is None else dev(rs, torch.uint8))
+        h, hT = L.gated_scan_forward(g, c, **kw)
+        m = [R.to64(x) for x in (g, c, hs, h0, sd, dT)]
+        ref, refT, bound, boundT = R.scan_forward(m[0], m[1], m[3], R.GIVEN, 1.0, ln, rs)
+        R.check(h, ref, bound + R.rounding(ref, dtype), "h")
+        R.check(hT, refT, boundT, "hT")
+        got = L.gated_scan_backward(g, c, hs, dh_seed=sd, dhT=dT, **kw)
+        refs, bounds = R.scan_backward(*m, R.GIVEN, 1.0, ln, rs)
+        for what, x, r, bd in zip(("dgate", "dcand", "dh0"), got, refs, bounds):
+            R.check(x, r, bd + (0 if what == "dh0" else R.rounding(r, dtype)), what)
+    assert L.last_device_status() == 0
