@@ -21,7 +21,7 @@
 // Measured, B200 (us; in brackets the bytes at the measured copy rate): T 2048, B 32, H 1024 in bf16 forward 119 (61), backward 191 (123);
 // 65536 steps of 1024 units in fp32 forward 253 (123); one step of 32 x 1024 4.3.  What bounds it: two warps on each scheduler that issue
 // dependent arithmetic (45 % of the issue slots, exponentials and reciprocals 39 % of theirs, DRAM 38 %); with given coefficients the first
-// takes 79.  Few columns: the chain of tiles, 0.1 us each at 512 tiles.
+// takes 80.  Few columns: the chain of tiles, 0.1 us each at 512 tiles.
 // Decoupled look-back is a published method (D. Merrill, M. Garland, "Single-pass parallel prefix scan with decoupled look-back", 2016).
 #pragma once
 #include <type_traits>
@@ -250,9 +250,9 @@ __device__ __forceinline__ float2 through(float2 p, float2 q, bool cut) { return
 // A product of coefficients says what becomes of a state of any size only as far as fp32 has room for it.
 //  * Coefficients of at most 1 in size: one that underflows is right to 2^-149 of the state.  It stays at the smallest number of its sign, so that
 //    an infinite state remains infinite.
-//  * Others (STRICT): an overflow, or digits lost below 2^-126 that coefficients above 1 may bring back, make it useless (3^128 times a state of
-//    zero is zero, inf times zero is NaN): kLost.  Such a piece is walked from its own first state instead.  Only the product of a whole tile whose
-//    coefficients are at most 1 may still underflow as above.  A zero among the coefficients makes it zero, whatever the others' product was.
+//  * In a tile where some are above 1 (STRICT): an overflow, or digits lost below 2^-126 that coefficients above 1 may bring back, make it useless
+//    (3^128 times a state of zero is zero, inf times zero is NaN): kLost.  Such a piece is walked from its own first state instead.
+//  * A zero among given coefficients makes it zero, whatever the others' product was.
 constexpr float kSteady = 1.001f;              // (roundings above 1 bring nothing back)
 constexpr float kLeast = 1.17549435e-38f, kMost = 3.4028235e38f;
 constexpr float kLost = INFINITY;              // in the place of a product (never published)
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
       A = s == 0 ? ca[s] : ca[s] * A;
       h = step(s, h);
     }
-    bool odd = false, lost = false;            // a coefficient above 1, or a product out of range; a column's product is not to be had
+    bool big = false, lost = false;            // a coefficient above 1 (or NaN); a column's product is not to be had
     if (ODD && cut && fresh_now != 0u) {
       A = V::all(__uint_as_float(0x7fc00000u));
     } else if constexpr (STRICT) {
@@ -639,8 +639,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
       float least = A.at(0);
 #pragma unroll
       for (int v = 0; v < VC; v += 2) least = smallest_nan(least, A.at(v), A.at(v + 1 < VC ? v + 1 : v));
-      if (!(fmaxf(most[0], most[1]) <= kSteady && least >= kLeast)) {
-        odd = true;
+      big = !(fmaxf(most[0], most[1]) <= kSteady) || least != least;
+      if (big) {
         constexpr float kUp = S == 8 ? 32768.f : 128.f;      // S coefficients up to that, and down to its inverse, leave the product in range
         static_assert(S == 8 || S == 16, "S powers of kUp are 2^120, or 2^112");
 #pragma unroll
@@ -650,6 +650,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
           for (int s = 0; s < S; ++s) { up = max_nan(up, fabsf(ca[s].at(v))); down = fminf(down, fabsf(ca[s].at(v))); }
           if (up <= kMost && down == 0.f) A.at(v) = 0.f;
           else if (!(up <= kSteady ? fabsf(A.at(v)) >= kLeast : up <= kUp && down * kUp >= 1.f)) A.at(v) = kLost, lost = true;
+        }
+      } else if (least < kLeast) {
+#pragma unroll
+        for (int v = 0; v < VC; ++v) {
+          if (A.at(v) == 0.f) {
+            float down = kMost;
+#pragma unroll
+            for (int s = 0; s < S; s += 2) down = smallest_nan(down, ca[s].at(v), ca[s + 1].at(v));
+            if (down > 0.f) A.at(v) = kept(A.at(v));
+          }
         }
       }
     } else {
@@ -669,11 +679,23 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
         for (int v = 0; v < VC; ++v) early[v] = word_of(__uint_as_float(early[v]));
       }
     }
-    // The only meeting of the block's warps, as a rule: the arrays are used in turn.  checks: some piece is odd; walk: some has to be walked.
-    bool checks = false, walk = false;
+    // The only meeting of the block's warps, as a rule: the arrays are used in turn.  grows: a coefficient of the tile is above 1, so that pieces that
+    // underflow are of no use either; walk: some piece has to be walked.
+    bool grows = false, walk = false;
     if constexpr (STRICT) {
-      checks = __syncthreads_or(odd);
-      if (checks) walk = __syncthreads_or(lost);
+      grows = __syncthreads_or(big);
+      if (grows) {
+        if (!big) {
+#pragma unroll
+          for (int v = 0; v < VC; ++v) {
+            if (fabsf(A.at(v)) < kLeast && A.at(v) != 0.f) {
+              pair[buf][warp][lane * VC + v].x = A.at(v) = kLost;
+              lost = true;
+            }
+          }
+        }
+        walk = __syncthreads_or(lost);
+      }
     } else {
       __syncthreads();
     }
@@ -692,20 +714,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) scan_tile_kernel(const __grid_
 #pragma unroll
       for (int v = 0; v < VC; ++v) {
         float& p = whole[v].x;
-        if (!checks) {
+        if (!STRICT) {
           p = kept(p);
-        } else if (p == p) {
-          float q = 1.f;
-          bool zero = false, out = false, large = false;
-#pragma unroll 1
+        } else if (grows || p == 0.f) {
+          float up = 0.f, down = kMost;
+#pragma unroll
           for (int w = 0; w < kWarps; ++w) {
             const float x = pair[buf][w][lane * VC + v].x;
-            zero = zero || x == 0.f;
-            large = large || fabsf(x) > kSteady;
-            q *= x;
-            out = out || !(fabsf(q) >= kLeast && fabsf(q) <= kMost);
+            up = largest(up, x, x);
+            down = smallest_nan(down, x, x);
           }
-          p = zero ? 0.f : large && out ? kLost : kept(p);
+          if (down == 0.f) {                   // (all of them are finite)
+            p = 0.f;
+          } else if (up <= kSteady) {
+            p = kept(p);
+          } else if (down == down && !(up <= 32768.f && down * 32768.f >= 1.f)) {
+            float q = 1.f;
+            bool out = false;
+#pragma unroll 1
+            for (int w = 0; w < kWarps; ++w) {
+              q *= pair[buf][w][lane * VC + v].x;
+              out = out || !(fabsf(q) >= kLeast && fabsf(q) <= kMost);
+            }
+            if (out) p = kLost;
+          }
         }
       }
     };
